@@ -26,8 +26,8 @@ PEAKS_SOURCE = "peaks.hip"
 PEAKS_PATH = os.path.join(PKG, "libvase_peaks.so")
 
 SOURCES = ["abi.hip", "score.hip", "score_f32.hip", "select.hip", "compact.hip", "decode.hip", "dkv.hip",
-           "quant.hip", "order.hip"]
-HEADERS = ["vase_internal.hpp"]
+           "quant.hip", "order.hip", "page_abi.hip", "page_attn.hip", "page_state.hip"]
+HEADERS = ["vase_internal.hpp", "page_internal.hpp"]
 ARCH = "gfx950"
 
 
