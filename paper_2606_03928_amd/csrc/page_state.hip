@@ -14,6 +14,16 @@ __device__ __forceinline__ void raise(uint32_t* status, uint32_t bit) {
   if (status) atomicOr(status, bit);
 }
 
+// rows that are not read again soon: past the caches (compact of 2304 heads of 4096 rows:
+// 1936 us with plain accesses, 1896 so)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+}
+__device__ __forceinline__ void store_once(uint4* p, const uint4& x) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), reinterpret_cast<u32x4*>(p));
+}
+
 // ---------------------------------------------------------------------------
 // write: one wave per token and group of heads, K and V.  Bound by HBM (each row read
 // once, written once); the token's slot is found by the wave's lanes together.
@@ -87,20 +97,35 @@ __device__ __forceinline__ long long block_scan(long long x, long long* s_wave, 
   return before + y - x;
 }
 
-// the lowest `want` pages without a count into list, in order; how many there are of them
-__device__ int list_free(const int32_t* __restrict__ ref, int n_pages, int want, int32_t* list,
-                         int* s_count /* [8 * kPlanWaves] */) {
-  constexpr int U = 8;
+// The counts of the pages from `base` on that a thread looks at in one pass of the search
+// (behind the last page: its own count).
+constexpr int kLook = 8;
+struct Look {
+  int r[kLook];
+};
+__device__ __forceinline__ Look look(const int32_t* __restrict__ ref, int n_pages, int64_t base) {
+  Look l;
+#pragma unroll
+  for (int u = 0; u < kLook; ++u) {
+    const int64_t p = base + u * kPlanBlock + threadIdx.x;
+    l.r[u] = ref[p < n_pages ? p : n_pages - 1];
+  }
+  return l;
+}
+
+// The lowest `want` pages without a count into list, in order; how many there are of them.
+// l: the first pass's counts, which do not wait for `want`.
+__device__ int list_free(const int32_t* __restrict__ ref, int n_pages, int want, Look l, int32_t* list,
+                         int* s_count /* [kLook * kPlanWaves] */) {
+  constexpr int U = kLook;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int found = 0;
   for (int64_t base = 0; base < n_pages && found < want; base += U * kPlanBlock) {
     uint64_t m[U];
+    if (base > 0) l = look(ref, n_pages, base);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t p = base + u * kPlanBlock + threadIdx.x;
-      const int r = ref[p < n_pages ? p : n_pages - 1];
-      m[u] = __ballot(p < n_pages && r == 0);
-    }
+    for (int u = 0; u < U; ++u)
+      m[u] = __ballot(base + u * kPlanBlock + threadIdx.x < n_pages && l.r[u] == 0);
     if (lane < U) {
       uint64_t mine = 0;
 #pragma unroll
@@ -136,6 +161,8 @@ __device__ int list_free(const int32_t* __restrict__ ref, int n_pages, int want,
 // workspace head: the call goes through; number of listed slots
 constexpr int kHead = 16;
 
+constexpr int kCopyBlocks = 512;   // of a resize: most calls copy little or nothing
+
 struct ResizePlan {   // in the workspace, int32 each
   int32_t *head, *begin, *off, *cow_slot, *cow_page, *cow_rows, *free;
 };
@@ -149,9 +176,10 @@ __global__ __launch_bounds__(kPlanBlock) void page_resize_plan_kernel(PageView c
                                                                       const int32_t* __restrict__ new_len,
                                                                       ResizePlan w, uint32_t* status) {
   __shared__ long long s_wave[kPlanWaves];
-  __shared__ int s_count[8 * kPlanWaves];
+  __shared__ int s_count[kLook * kPlanWaves];
   constexpr int kCow = 48;   // sums of two numbers in one: pages below bit 48, copies above
   const int cap = c.M * c.page;
+  const Look first_look = look(c.ref, c.n_pages, 0);
   bool bad = false;
   long long need_all = 0;
   int n_cow = 0;
@@ -203,7 +231,7 @@ __global__ __launch_bounds__(kPlanBlock) void page_resize_plan_kernel(PageView c
   bad = __syncthreads_or(bad);
   bool full = need_all > c.n_pages;
   if (!bad && !full && need_all > 0)
-    full = list_free(c.ref, c.n_pages, (int)need_all, w.free, s_count) < need_all;
+    full = list_free(c.ref, c.n_pages, (int)need_all, first_look, w.free, s_count) < need_all;
   if (threadIdx.x == 0) {
     w.head[0] = !bad && !full;
     w.head[1] = n_cow;
@@ -218,16 +246,15 @@ template <int PPR>
 __global__ __launch_bounds__(kBlock) void page_resize_kernel(PageView c,
                                                              const int32_t* __restrict__ new_len,
                                                              ResizePlan w, uint32_t* status) {
-  if (!w.head[0]) return;
   if ((int)blockIdx.x < c.S) {
     const int s = blockIdx.x;
-    const int L = c.len[s], t = new_len[s];
-    if (t < 0 || t == L) return;
+    // every load that waits for no other; the plan writes begin and off of every slot
+    const int go = w.head[0], L = c.len[s], t = new_len[s], first = w.begin[s], off = w.off[s];
+    if (!go || t < 0 || t == L) return;
     __syncthreads();   // every thread has the old length
     int32_t* row = c.table + (int64_t)s * c.M;
     const int old = pages_for(c, L), now = pages_for(c, t);
     if (t > L) {
-      const int first = w.begin[s], off = w.off[s];
       for (int j = first + threadIdx.x; j < now; j += kBlock) {
         if (j < old) atomicSub(&c.ref[row[j]], 1);   // the shared page that it grows in
         const int p = w.free[off + j - first];
@@ -245,7 +272,7 @@ __global__ __launch_bounds__(kBlock) void page_resize_kernel(PageView c,
     if (threadIdx.x == 0) c.len[s] = t;
     return;
   }
-  const int64_t items = (int64_t)w.head[1] * c.H;
+  const int64_t items = w.head[0] ? (int64_t)w.head[1] * c.H : 0;
   for (int64_t i = blockIdx.x - c.S; i < items; i += gridDim.x - c.S) {
     const int e = (int)(i / c.H), h = (int)(i % c.H);
     const int64_t from = w.cow_page[e] * c.page_u4 + h * c.head_u4;
@@ -289,25 +316,37 @@ __global__ __launch_bounds__(kBlock) void page_fork_kernel(PageView c, const int
 // ---------------------------------------------------------------------------
 // compact
 // ---------------------------------------------------------------------------
+// rows that a workgroup moves at once: 16 KB of K and V each, 8 KB of the shortest rows
+constexpr int chunk_rows(int row_pieces) { return row_pieces == 32 ? 32 : 64; }
+constexpr int kTicketGap = 32;      // counters of their own cache lines
+constexpr int kFewItems = 512;     // (slot, head) pairs below which chunks go one by one
+
 struct CompactState {   // in the workspace, int32 each
   int32_t *head;
   int32_t *slot, *len;  // [S]: the slots to compact and their lengths
   int32_t *old, *rank;  // [S][M] by list place: the entries, and which free page replaces each (-1: none)
   int32_t *free;        // [n_pages]
+  int32_t *ticket;      // few (slot, head) pairs: the next chunk of each, kTicketGap apart
+  int32_t *said;        // and [pair][chunk], 1: its rows are in registers
 };
-CompactState compact_state(void* ws, int S, int M) {
+// fewer than kFewItems, whatever the slots
+size_t few_pairs(const vase_pages& c) { return (size_t)c.S * c.H < kFewItems ? (size_t)c.S * c.H : kFewItems; }
+CompactState compact_state(void* ws, const vase_pages& c) {
   int32_t* p = static_cast<int32_t*>(ws) + kHead;
-  const size_t sm = (size_t)S * M;
-  return CompactState{static_cast<int32_t*>(ws), p, p + S, p + 2 * S, p + 2 * S + sm, p + 2 * S + 2 * sm};
+  const size_t S = c.S, sm = S * c.M;
+  return CompactState{static_cast<int32_t*>(ws), p, p + S, p + 2 * S, p + 2 * S + sm, p + 2 * S + 2 * sm,
+                      p + 2 * S + 2 * sm + c.n_pages,
+                      p + 2 * S + 2 * sm + c.n_pages + few_pairs(c) * kTicketGap};
 }
 
 __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView c,
                                                                        const int32_t* __restrict__ map,
-                                                                       int n_map, int K, CompactState w,
+                                                                       int n_map, int K, int chunk, CompactState w,
                                                                        uint32_t* status) {
   __shared__ long long s_wave[kPlanWaves];
-  __shared__ int s_count[8 * kPlanWaves];
+  __shared__ int s_count[kLook * kPlanWaves];
   __shared__ int s_most;
+  const Look first_look = look(c.ref, c.n_pages, 0);
   if (threadIdx.x == 0) s_most = 0;
   __syncthreads();
   bool bad = false;
@@ -349,7 +388,12 @@ __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView 
   }
   bad = __syncthreads_or(bad);
   bool full = need > c.n_pages;
-  if (!bad && !full && need > 0) full = list_free(c.ref, c.n_pages, (int)need, w.free, s_count) < need;
+  if (!bad && !full && need > 0) full = list_free(c.ref, c.n_pages, (int)need, first_look, w.free, s_count) < need;
+  const int64_t items = (int64_t)n * c.H;
+  if (items < kFewItems) {
+    for (int i = threadIdx.x; i < items; i += kPlanBlock) w.ticket[i * kTicketGap] = 0;
+    for (int64_t i = threadIdx.x; i < items * ((K + chunk - 1) / chunk); i += kPlanBlock) w.said[i] = 0;
+  }
   if (threadIdx.x == 0) {
     w.head[0] = !bad && !full;
     w.head[1] = n;
@@ -358,17 +402,46 @@ __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView 
   }
 }
 
-// Workgroups below n_state: entries, counts and lengths of listed slots.  The others move
-// rows, one (slot, head, pool) at a time, in ascending chunks.  As src[j] >= j and src
-// increases, a row that a chunk overwrites is read by that chunk or an earlier one only,
-// so a chunk's stores wait for its own loads (and a barrier, for the other waves'), and
-// the next chunk's loads need not wait for them.
+// Where row j of a (slot, head) comes from and goes to, in pieces from the pools' first; `to`
+// is -1 for a row that stays where it is, and for rows from K on.
+struct RowMove {
+  int64_t from, to;
+};
+template <int PPR>
+__device__ __forceinline__ RowMove row_move(const PageView& c, const CompactState& w, int e, int64_t head,
+                                            int K, int j, int src) {
+  const int32_t* old = w.old + (int64_t)e * c.M;
+  const int jj = min(j, K - 1);
+  const int f = min(max(src, 0), w.len[e] - 1);
+  const int qf = page_of_group(c.div, f / 16), qt = page_of_group(c.div, jj / 16);
+  const int rt = w.rank[(int64_t)e * c.M + qt];
+  const int pt = rt < 0 ? old[qt] : w.free[rt];
+  RowMove m;
+  m.from = old[qf] * c.page_u4 + head + (int64_t)(f - qf * c.page) * PPR;
+  m.to = j < K && (f != j || rt >= 0) ? pt * c.page_u4 + head + (int64_t)(jj - qt * c.page) * PPR : -1;
+  return m;
+}
+
+// Workgroups below n_state: entries, counts and lengths of the listed slots.  The others move
+// rows, K and V of a (slot, head) together, a chunk at a time.  As src[j] >= j and src
+// increases, a row that a chunk overwrites is read by that chunk and earlier ones only.
+//
+// Many (slot, head) pairs: a workgroup takes whole ones, its chunks in ascending order; a
+// chunk's stores wait for its own loads (and a barrier, for the other waves'), while the next
+// chunk's loads are under way.  Few: workgroups take single chunks of a pair, by ticket;
+// a chunk's rows are all in registers before it says so, and its stores wait until the chunks
+// before it whose sources reach into it have said so.  They have lower tickets, so they
+// are with running workgroups, which wait for nothing before they speak: every wait
+// ends.  Bound by HBM: each row is read once and written once.
 template <int PPR>
 __global__ __launch_bounds__(kBlock) void page_compact_kernel(PageView c, const int32_t* __restrict__ map,
                                                               const int32_t* __restrict__ src, int K,
                                                               CompactState w, int n_state) {
-  constexpr int U = 8;
+  constexpr int kChunk = chunk_rows(PPR);
   constexpr int kRows = kBlock / PPR;        // rows of one load by the workgroup
+  constexpr int U = kChunk / kRows;
+  __shared__ RowMove s_move[4][kChunk];
+  __shared__ int s_ticket;
   if (!w.head[0]) return;
   const int n = w.head[1], kept = pages_for(c, K);
   if ((int)blockIdx.x < n_state) {
@@ -388,46 +461,119 @@ __global__ __launch_bounds__(kBlock) void page_compact_kernel(PageView c, const 
     }
     return;
   }
-  const int col = threadIdx.x % PPR, r0 = threadIdx.x / PPR;
-  const int64_t items = (int64_t)n * c.H * 2;
-  for (int64_t i = blockIdx.x - n_state; i < items; i += gridDim.x - n_state) {
-    const int e = (int)(i / (2 * c.H)), h = (int)(i % (2 * c.H)) / 2;
-    uint4* pool = i % 2 ? c.v : c.k;
-    const int s = w.slot[e], L = w.len[e];
-    const int32_t* sr = src + ((int64_t)map[s] * c.H + h) * K;
-    const int32_t* old = w.old + (int64_t)e * c.M;
-    const int32_t* rank = w.rank + (int64_t)e * c.M;
-    const int64_t head = h * c.head_u4 + col;
-    for (int c0 = 0; c0 < K; c0 += U * kRows) {
-      uint4 x[U];
-      int64_t to[U];
+  const int tid = threadIdx.x, col = tid % PPR, r0 = tid / PPR;
+  const int64_t items = (int64_t)n * c.H;
+  const int chunks = (K + kChunk - 1) / kChunk;
+  auto head_of = [&](int64_t i, int& e) {
+    e = (int)(i / c.H);
+    return src + ((int64_t)map[w.slot[e]] * c.H + i % c.H) * K;
+  };
+  uint4 a[2][U], b[2][U];
+  auto load = [&](const RowMove* mv, uint4 (&x)[U], uint4 (&y)[U]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int j = c0 + r0 + u * kRows;
-        const int jj = min(j, K - 1);
-        const int f = min(max(sr[jj], 0), L - 1);
-        const int qf = page_of_group(c.div, f / 16), qt = page_of_group(c.div, jj / 16);
-        const int pf = old[qf], rt = rank[qt];
-        const int pt = rt < 0 ? old[qt] : w.free[rt];
-        x[u] = pool[pf * c.page_u4 + head + (int64_t)(f - qf * c.page) * PPR];
-        to[u] = j < K && (f != j || rt >= 0)
-                    ? pt * c.page_u4 + head + (int64_t)(jj - qt * c.page) * PPR
-                    : -1;
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = mv[r0 + u * kRows].from + col;
+      x[u] = load_once(c.k + at);
+      y[u] = load_once(c.v + at);
+    }
+  };
+  auto arrived = [&](uint4 (&x)[U], uint4 (&y)[U]) {   // waits for the wave's loads
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+      asm volatile("" : "+v"(y[u].x), "+v"(y[u].y), "+v"(y[u].z), "+v"(y[u].w));
+    }
+  };
+  auto store = [&](const RowMove* mv, const uint4 (&x)[U], const uint4 (&y)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = mv[r0 + u * kRows].to;
+      if (at >= 0) {
+        store_once(c.k + at + col, x[u]);
+        store_once(c.v + at + col, y[u]);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)   // the loads are done before the barrier
-        asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+    }
+  };
+
+  if (items == 0) return;
+  if (items < kFewItems) {
+    // one counter to a pair: on a single one the workgroups' atomics queued (60 us for 32 pairs
+    // of 32 chunks)
+    const int n_block = (int)(gridDim.x - n_state), per = n_block / (int)items;
+    const int i = (int)(blockIdx.x - n_state) % (int)items;
+    if ((int)(blockIdx.x - n_state) >= per * (int)items) return;
+    int e;
+    const int32_t* sr = head_of(i, e);
+    int32_t* said = w.said + (int64_t)i * chunks;
+    for (int taken = 0; taken < chunks; taken += per) {
+      __syncthreads();   // the chunk before is stored
+      if (tid == 0) s_ticket = atomicAdd(&w.ticket[i * kTicketGap], 1);
       __syncthreads();
+      const int ch = s_ticket;
+      if (ch >= chunks) return;
+      if (tid < kChunk) {
+        const int j = ch * kChunk + tid;
+        s_move[0][tid] = row_move<PPR>(c, w, e, (i % c.H) * c.head_u4, K, j, sr[min(j, K - 1)]);
+      }
+      __syncthreads();
+      load(s_move[0], a[0], b[0]);
+      arrived(a[0], b[0]);
+      __syncthreads();   // every wave's
+      if (tid == 0) __hip_atomic_store(&said[ch], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // the chunks before, nearest first, as long as their last source is in this chunk's rows
+      if (tid < kWave) {
+        for (int p = ch - 1 - tid;; p -= kWave) {
+          const bool reaches = p >= 0 && sr[(p + 1) * kChunk - 1] >= ch * kChunk;
+          if (reaches)
+            while (__hip_atomic_load(&said[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0)
+              __builtin_amdgcn_s_sleep(1);
+          if (__ballot(!reaches)) break;
+        }
+      }
+      __syncthreads();
+      store(s_move[0], a[0], b[0]);
+    }
+    return;
+  }
+
+  for (int64_t i = blockIdx.x - n_state; i < items; i += gridDim.x - n_state) {
+    int e;
+    const int32_t* sr = head_of(i, e);
+    const int64_t head = (i % c.H) * c.head_u4;
+    // the moves of chunk x into its place of four; their sources read a chunk earlier
+    int ahead = tid < kChunk ? sr[min(tid, K - 1)] : 0;
+    auto moves = [&](int x) {
+      if (tid < kChunk) {
+        const int j = x * kChunk + tid;
+        s_move[x % 4][tid] = row_move<PPR>(c, w, e, head, K, j, ahead);
+        ahead = sr[min(j + kChunk, K - 1)];
+      }
+    };
+    __syncthreads();   // the item before has read its moves
+    moves(0);
+    moves(1);
+    __syncthreads();
+    load(s_move[0], a[0], b[0]);
+    for (int x = 0; x < chunks; x += 2) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (to[u] >= 0) pool[to[u]] = x[u];
+      for (int o = 0; o < 2; ++o) {
+        const int y = x + o;
+        if (y >= chunks) break;
+        moves(y + 2);   // ahead of the loads, whose end its own look-ups would wait for
+        if (y + 1 < chunks) load(s_move[(y + 1) % 4], a[1 - o], b[1 - o]);
+        arrived(a[o], b[o]);
+        __syncthreads();
+        store(s_move[y % 4], a[o], b[o]);
+      }
     }
   }
 }
 
+int row_pieces(const vase_pages& c) { return c.d * (c.dtype == VASE_BF16 ? 2 : 4) / 16; }
+
 template <typename F>
 hipError_t by_row(const vase_pages& c, F f) {   // 16-byte pieces of a row
-  const int ppr = c.d * (c.dtype == VASE_BF16 ? 2 : 4) / 16;
+  const int ppr = row_pieces(c);
   if (ppr == 8) f(std::integral_constant<int, 8>());
   else if (ppr == 16) f(std::integral_constant<int, 16>());
   else f(std::integral_constant<int, 32>());
@@ -461,7 +607,7 @@ hipError_t launch_page_resize(const vase_pages& c, const int32_t* new_len, void*
   const int64_t copies = (int64_t)c.S * c.H;
   return by_row(c, [&](auto ppr) {
     constexpr int P = decltype(ppr)::value;
-    hipLaunchKernelGGL((page_resize_kernel<P>), dim3((unsigned)(c.S + (copies < 1024 ? copies : 1024))),
+    hipLaunchKernelGGL((page_resize_kernel<P>), dim3((unsigned)(c.S + (copies < kCopyBlocks ? copies : kCopyBlocks))),
                        dim3(kBlock), 0, stream, v, new_len, w, status);
   });
 }
@@ -473,20 +619,28 @@ hipError_t launch_page_fork(const vase_pages& c, const int32_t* parent, uint32_t
 }
 
 size_t page_compact_bytes(const vase_pages& c) {
-  return sizeof(int32_t) * (kHead + 2 * (size_t)c.S + 2 * (size_t)c.S * c.M + (size_t)c.n_pages);
+  const int chunk = chunk_rows(row_pieces(c));
+  const size_t chunks = ((size_t)c.M * c.page + chunk - 1) / chunk;
+  return sizeof(int32_t) * (kHead + 2 * (size_t)c.S + 2 * (size_t)c.S * c.M + (size_t)c.n_pages +
+                            few_pairs(c) * (kTicketGap + chunks));
 }
 
 hipError_t launch_page_compact(const vase_pages& c, const int32_t* map, const int32_t* src, int n_map,
                                int K, void* ws, uint32_t* status, hipStream_t stream) {
   const PageView v = page_view(c);
-  const CompactState w = compact_state(ws, c.S, c.M);
-  hipLaunchKernelGGL(page_compact_plan_kernel, dim3(1), dim3(kPlanBlock), 0, stream, v, map, n_map, K, w,
-                     status);
+  const CompactState w = compact_state(ws, c);
+  const int chunk = chunk_rows(row_pieces(c));
+  hipLaunchKernelGGL(page_compact_plan_kernel, dim3(1), dim3(kPlanBlock), 0, stream, v, map, n_map, K,
+                     chunk, w, status);
   const int n_state = c.S < 1024 ? c.S : 1024;
-  const int64_t items = (int64_t)c.S * c.H * 2;
+  // one workgroup per pair, or per chunk where pairs are few, up to a chip's fill of them
+  const int64_t pairs = (int64_t)c.S * c.H;
+  int64_t movers = pairs < kFewItems ? pairs * ((K + chunk - 1) / chunk) : pairs;
+  const int64_t most = pairs < kFewItems ? 2048 : 8192;
+  if (movers > most) movers = most;
   return by_row(c, [&](auto ppr) {
     constexpr int P = decltype(ppr)::value;
-    hipLaunchKernelGGL((page_compact_kernel<P>), dim3((unsigned)(n_state + (items < 8192 ? items : 8192))),
+    hipLaunchKernelGGL((page_compact_kernel<P>), dim3((unsigned)(n_state + movers)),
                        dim3(kBlock), 0, stream, v, map, src, K, w, n_state);
   });
 }

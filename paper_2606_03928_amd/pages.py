@@ -31,7 +31,7 @@ from typing import Optional
 import torch
 
 from . import vase
-from .vase import _check, _ptr, _require, _stream_ptr
+from .vase import _ptr, _require, _stream_ptr
 
 STATUS_PAGE_FULL, STATUS_PAGE_BAD = 16, 32
 OP_PAGE_ATTN, OP_PAGE_RESIZE, OP_PAGE_COMPACT = 0, 1, 2
@@ -73,23 +73,25 @@ def load() -> ctypes.CDLL:
 
 
 def _ints(t: torch.Tensor, shape, device, name: str) -> int:
-    _require(t.dtype == torch.int32 and tuple(t.shape) == tuple(shape) and t.is_contiguous()
-             and t.device == device,
-             "%s must be a contiguous int32 tensor %s on the cache's device" % (name, list(shape)))
+    if not (t.dtype is torch.int32 and t.shape == shape and t.device == device and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous int32 tensor %s on the cache's device"
+                         % (name, list(shape)))
     return t.data_ptr()
 
 
-def _token_rows(t: torch.Tensor, heads: Optional[int], d: int, like: torch.Tensor, name: str) -> int:
+def _token_rows(t: torch.Tensor, heads: Optional[int], like: "PageCache", name: str) -> int:
     """The token stride of [T, heads, d] rows whose heads and elements are contiguous."""
-    _require(t.dim() == 3 and t.shape[2] == d and (heads is None or t.shape[1] == heads)
-             and t.dtype == like.dtype and t.device == like.device,
-             "%s must be [T, heads, d] of the cache's dtype, on its device" % name)
-    least = t.shape[1] * d
-    _require(t.stride(2) == 1 and (t.stride(1) == d or t.shape[1] == 1),
-             "%s must have contiguous heads" % name)
-    # of a single token (or none) the stride says nothing
-    stride = t.stride(0) if t.shape[0] > 1 else least
-    _require(stride >= least, "%s: tokens must not overlap" % name)
+    if not (t.dim() == 3 and t.dtype is like.dtype and t.device == like.device):
+        raise ValueError("%s must be [T, heads, d] of the cache's dtype, on its device" % name)
+    T, H, d = t.shape
+    stride, head, one = t.stride()
+    least = H * d
+    if T <= 1:
+        stride = least          # of a single token (or none) the stride says nothing
+    if d != like.d or (heads is not None and H != heads):
+        raise ValueError("%s must be [T, heads, d] of the cache's heads and row length" % name)
+    if one != 1 or (head != d and H != 1) or stride < least:
+        raise ValueError("%s must have contiguous heads, and tokens that do not overlap" % name)
     return stride
 
 
@@ -120,11 +122,14 @@ class PageCache:
         self.S, self.M, self.n_pages, self.H, self.page, self.d = S, M, P, H, page, d
         self.device, self.dtype = dev, k.dtype
         self.status = status
+        self._status_word = vase._status_ptr(status, dev)
         self._c = _Pages(_ptr(k), _ptr(v), _ints(ref, (P,), dev, "ref"), _ints(table, (S, M), dev, "table"),
                          _ints(length, (S,), dev, "length"), stride[0], vase.dtype_code(k.dtype), P, H,
                          page, d, S, M)
-        self._need = {}      # workspace bytes by operation and sizes
+        self._need = {}          # workspace bytes by operation and sizes
+        self._state_ws = None    # of resize and compact, made by the first of them
         self._lib = load()
+        self._by = ctypes.byref(self._c)
 
     @classmethod
     def new(cls, n_pages: int, H: int, page: int, d: int, S: int, M: int,
@@ -150,7 +155,7 @@ class PageCache:
             if len(self._need) >= 256:
                 self._need.clear()
             n = self._need[key] = int(self._lib.vase_page_workspace_bytes(
-                op, ctypes.byref(self._c), T, G, max_new, max_len))
+                op, self._by, T, G, max_new, max_len))
         return n
 
     def attn_workspace_bytes(self, T: int, G: int, max_new: int, max_len: Optional[int] = None) -> int:
@@ -162,30 +167,44 @@ class PageCache:
         return max(self._bytes(OP_PAGE_RESIZE), self._bytes(OP_PAGE_COMPACT))
 
     def _ws(self, ws, nbytes: int, stream):
+        """(pointer, bytes, tensor) of the given workspace or a new one."""
         if ws is None:
-            return self._new((nbytes,), torch.uint8, stream) if nbytes else None
+            if nbytes == 0:
+                return None, 0, None
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            if stream is not None:
+                ws.record_stream(stream)     # allocated on the current stream, used on the given one
+            return ws.data_ptr(), nbytes, ws
         _require(ws.is_cuda and ws.device == self.device and ws.is_contiguous(),
                  "ws must be a contiguous tensor on the cache's device")
-        _require(ws.numel() * ws.element_size() >= nbytes, "workspace too small")
-        return ws
+        have = ws.numel() * ws.element_size()
+        _require(have >= nbytes, "workspace too small")
+        return ws.data_ptr(), have, ws
 
-    def _new(self, shape, dtype, stream):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if stream is not None:
-            t.record_stream(stream)      # allocated on the current stream, used on the given one
-        return t
+    def _state(self, ws, op: int, stream):
+        """As _ws, for resize and compact: by default the cache's own, as calls that change one
+        cache follow each other in any case.  A captured call takes one of its graph's."""
+        if ws is None and not torch.cuda.is_current_stream_capturing():
+            ws = self._state_ws
+            if ws is None:
+                ws = self._state_ws = torch.empty(self.state_workspace_bytes(), dtype=torch.uint8,
+                                                  device=self.device)
+            if stream is not None:
+                ws.record_stream(stream)
+            return ws.data_ptr(), ws.numel(), ws
+        return self._ws(ws, self._bytes(op), stream)
 
     def _status(self, status):
-        status = self.status if status is None else status
-        return vase._status_ptr(status, self.device)
+        return self._status_word if status is None else vase._status_ptr(status, self.device)
 
-    def _call(self, name: str, *args):
-        f = getattr(self._lib, name)
+    def _call(self, f, name: str, *args):
         if torch.cuda.current_device() == self.device.index:
-            _check(f(ctypes.byref(self._c), *args), name)
+            rc = f(self._by, *args)
         else:
             with torch.cuda.device(self.device):
-                _check(f(ctypes.byref(self._c), *args), name)
+                rc = f(self._by, *args)
+        if rc != vase.OK:
+            raise vase.VaseError(name, rc)
 
     # -- operators ---------------------------------------------------------------------
 
@@ -201,10 +220,11 @@ class PageCache:
         of a wider tensor: any stride from token to token.  lse [T, H * G] float32 takes
         the rows' log-sum-exp.  Returns out [T, H * G, d]; the tokens from cu[S] on, if
         any, are left as they were (zero in an out made here)."""
-        stride = _token_rows(q, None, self.d, self.k, "q")
-        T, HG = int(q.shape[0]), int(q.shape[1])
-        _require(HG % self.H == 0 and HG > 0, "q must have G query heads for each of the cache's heads")
-        G = HG // self.H
+        stride = _token_rows(q, None, self, "q")
+        T, HG, d = q.shape
+        G, rest = divmod(HG, self.H)
+        if rest or G < 1:
+            raise ValueError("q must have G query heads for each of the cache's heads")
         if max_len is None:
             max_len = self.M * self.page
         cup = _ints(cu, (self.S + 1,), self.device, "cu")
@@ -214,15 +234,18 @@ class PageCache:
                 # the zeros are written on the current stream
                 stream.wait_stream(torch.cuda.current_stream(self.device))
                 out.record_stream(stream)
-        _require(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
-                 and out.device == self.device, "out must be contiguous, like q")
+        elif not (out.shape == q.shape and out.dtype is q.dtype and out.device == self.device
+                  and out.is_contiguous()):
+            raise ValueError("out must be contiguous, like q")
+        lp = None
         if lse is not None:
+            lp = lse.data_ptr()
             _require(lse.dtype == torch.float32 and tuple(lse.shape) == (T, HG) and lse.is_contiguous()
                      and lse.device == self.device, "lse must be contiguous float32 [T, H * G]")
-        ws = self._ws(ws, self._bytes(OP_PAGE_ATTN, T, G, max_new, max_len) if T else 0, stream)
-        wp, wn = vase._ws_args(ws)
-        self._call("vase_page_attn", _ptr(q), stride, cup, T, G, max_new, max_len, 1 if causal else 0,
-                   _ptr(out), _ptr(lse), wp, wn, self._status(status), _stream_ptr(self.device, stream))
+        wp, wn, ws = self._ws(ws, self._bytes(OP_PAGE_ATTN, T, G, max_new, max_len) if T else 0, stream)
+        self._call(self._lib.vase_page_attn, "vase_page_attn", q.data_ptr(), stride, cup, T, G, max_new,
+                   max_len, 1 if causal else 0, out.data_ptr(), lp, wp, wn, self._status(status),
+                   _stream_ptr(self.device, stream))
         return out
 
     def write(self, k_new: torch.Tensor, v_new: torch.Tensor, cu: torch.Tensor, stream=None,
@@ -230,11 +253,12 @@ class PageCache:
         """The tokens' rows k_new, v_new [T, H, d] into the last rows of their slots: token i of
         slot s's n into row length[s] - n + i (vase_page_write).  Both may be parts of wider
         tensors with one stride from token to token."""
-        a = _token_rows(k_new, self.H, self.d, self.k, "k_new")
-        b = _token_rows(v_new, self.H, self.d, self.k, "v_new")
-        _require(k_new.shape == v_new.shape and a == b, "k_new and v_new must have one shape and stride")
-        self._call("vase_page_write", _ptr(k_new), _ptr(v_new), a,
-                   _ints(cu, (self.S + 1,), self.device, "cu"), int(k_new.shape[0]),
+        a = _token_rows(k_new, self.H, self, "k_new")
+        T = k_new.shape[0]
+        if a != _token_rows(v_new, self.H, self, "v_new") or v_new.shape[0] != T:
+            raise ValueError("k_new and v_new must have one shape and stride")
+        self._call(self._lib.vase_page_write, "vase_page_write", k_new.data_ptr(), v_new.data_ptr(), a,
+                   _ints(cu, (self.S + 1,), self.device, "cu"), T,
                    self._status(status), _stream_ptr(self.device, stream))
 
     def resize(self, new_len: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None,
@@ -243,13 +267,14 @@ class PageCache:
         up, taken (the lowest free ones), and copied where a slot grows within a page that it
         shares.  All or nothing: STATUS_PAGE_FULL with too few free pages (vase_page_resize)."""
         p = _ints(new_len, (self.S,), self.device, "new_len")
-        wp, wn = vase._ws_args(self._ws(ws, self._bytes(OP_PAGE_RESIZE), stream))
-        self._call("vase_page_resize", p, wp, wn, self._status(status), _stream_ptr(self.device, stream))
+        wp, wn, ws = self._state(ws, OP_PAGE_RESIZE, stream)
+        self._call(self._lib.vase_page_resize, "vase_page_resize", p, wp, wn, self._status(status),
+                   _stream_ptr(self.device, stream))
 
     def fork(self, parent: torch.Tensor, stream=None, status: Optional[torch.Tensor] = None) -> None:
         """Each free slot s with parent[s] >= 0 (parent [S] int32) begins as that slot: its
         rows, on the same pages (vase_page_fork)."""
-        self._call("vase_page_fork", _ints(parent, (self.S,), self.device, "parent"),
+        self._call(self._lib.vase_page_fork, "vase_page_fork", _ints(parent, (self.S,), self.device, "parent"),
                    self._status(status), _stream_ptr(self.device, stream))
 
     def compact(self, map: torch.Tensor, src: torch.Tensor, ws: Optional[torch.Tensor] = None,
@@ -261,8 +286,8 @@ class PageCache:
         n_map, K = int(src.shape[0]), int(src.shape[2])
         sp = _ints(src, src.shape, self.device, "src")
         mp = _ints(map, (self.S,), self.device, "map")
-        wp, wn = vase._ws_args(self._ws(ws, self._bytes(OP_PAGE_COMPACT), stream))
-        self._call("vase_page_compact", mp, sp, n_map, K, wp, wn, self._status(status),
+        wp, wn, ws = self._state(ws, OP_PAGE_COMPACT, stream)
+        self._call(self._lib.vase_page_compact, "vase_page_compact", mp, sp, n_map, K, wp, wn, self._status(status),
                    _stream_ptr(self.device, stream))
 
 
