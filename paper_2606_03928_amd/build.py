@@ -44,6 +44,10 @@ def _flags(src: str):
          "-Wall", "-Wno-unused-function", "-I", INCLUDE, "-I", CSRC]
     if src in ("select.hip", "dkv.hip", "quant.hip"):
         f.append("-ffp-contract=off")
+    if src == "page_attn.hip":
+        # MFMA results that the VALU works on stay in VGPRs, whatever else a kernel
+        # holds in AGPRs
+        f += ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
     return f
 
 

@@ -75,8 +75,7 @@ int vase_page_attn(const vase_pages* c, const void* q, int64_t q_stride, const i
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(cu, 4))
     return VASE_ERR_INVALID_ARG;
   const vase::PageAttnPlan plan = vase::page_attn_plan(*c, T, G, max_new, max_len);
-  if ((int64_t)plan.n_tile * plan.split_t * c->H > 0x7fffffffLL ||
-      (int64_t)c->S * plan.split_f * c->H > 0x7fffffffLL || (int64_t)T * c->H * G > 0x7fffffffLL)
+  if ((int64_t)plan.n_tile * c->H > 0x7fffffffLL / plan.n_split || (int64_t)T * c->H * G > 0x7fffffffLL)
     return VASE_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || ws_bytes < plan.bytes || !aligned(ws, 16))) return VASE_ERR_WORKSPACE;
   return hip_status(vase::launch_page_attn(*c, q, q_stride, cu, T, G, causal, out, lse, ws, plan,

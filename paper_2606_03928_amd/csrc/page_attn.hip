@@ -9,9 +9,10 @@
 // between lanes or through LDS.
 //
 // Two kernels: page_tile_kernel takes 128 query rows to a workgroup and is bound by its
-// MFMAs and exponentials; page_few_kernel takes up to 16 (a token of decoding) and is
-// bound by the K and V rows it reads.  Both may split the keys into ranges, whose
-// partial (m, l, O) page_combine_kernel joins in range order.
+// MFMAs and exponentials; page_few_kernel takes 16 (a token of decoding) and is bound by
+// the K and V rows it reads.  Where workgroups would be too few or too uneven to fill the
+// chip, the keys are split, and partial (m, l, O) are joined in the order of their keys by a
+// launch behind: ranges of one length (few), equal shares of all tiles (tile).
 //
 // Masked keys take p = 0 by a select on the score, and V rows behind the slot's end are
 // zeroed where they are staged.  A later token's V row may hold an infinity or a NaN, which
@@ -21,11 +22,13 @@
 #include "page_internal.hpp"
 
 #include <type_traits>
+#include <utility>
 
 namespace vase {
 namespace {
 
 typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 pbf16x2 __attribute__((ext_vector_type(2)));
 typedef short ps16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short pu16x2 __attribute__((ext_vector_type(2)));
 typedef float pf32x8 __attribute__((ext_vector_type(8)));
@@ -33,6 +36,8 @@ typedef float pf32x16 __attribute__((ext_vector_type(16)));
 typedef float pf32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));   // 16 bytes of a row
 typedef __attribute__((address_space(3))) ps16x4 lds_s16x4;
+
+#define INLINE __attribute__((always_inline))   // of lambdas: what they capture stays in registers
 
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
@@ -50,10 +55,13 @@ struct AttnArgs {
   int causal;
   void* out;
   float* lse;
-  float *part_o, *part_ml; // [split][T][HG][D], [split][T][HG][2]
-  int n_tile, n_split, keys;
-  int few_split, few_keys; // combine: those of the few-row kernel
-  int split_rows;          // slots of up to so many rows are the other kernel's (tile: 0 none)
+  // partials.  few: [range][T][HG] of D and of 2; tile: [workgroup][2][128] likewise
+  float *part_o, *part_ml;
+  int32_t* sums;           // tile, shares: [n_tile + 1], the sums of the row tiles' key tiles
+  int n_tile;              // few: row tiles of 16 rows; tile: of 128
+  int n_split, keys;       // few: key ranges
+  int by_slot;             // few: a slot's rows are one row tile
+  int shares;              // tile: workgroups that share the work (0: one to a row tile and head)
   float scale_log2;
   uint32_t* status;
 };
@@ -72,8 +80,15 @@ struct Span {
   }
 };
 
-// Where the 16-row groups of a slot lie: lane l holds the offset (in pieces, from the pool's
-// first) of group g0 + l of head h, 64 groups at a time.
+// Row tiles of R rows: those of slot s begin at number floor(cu[s] G / R) + s, which leaves
+// room for all of its rows, so that a tile's slot is found in cu alone.
+template <int R>
+__device__ __forceinline__ int first_tile(const AttnArgs& a, int s) {
+  return (int)((int64_t)min(max(a.cu[s], 0), a.T) * a.G / R) + s;
+}
+
+// Where the 16-row groups of a slot lie: lane l holds the address of group g0 + l of head h in
+// the K pool, 64 groups at a time.
 template <int PPR>
 struct GroupBases {
   uint32_t lo, hi;
@@ -87,7 +102,8 @@ struct GroupBases {
       if (a.status) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
       p = 0;
     }
-    const uint64_t at = (uint64_t)(p * a.c.page_u4 + h * a.c.head_u4 + (int64_t)(gl * 16 - q * a.c.page) * PPR);
+    const uint64_t at = reinterpret_cast<uint64_t>(
+        a.c.k + (p * a.c.page_u4 + h * a.c.head_u4 + (int64_t)(gl * 16 - q * a.c.page) * PPR));
     lo = (uint32_t)at;
     hi = (uint32_t)(at >> 32);
     g0 = g;
@@ -96,11 +112,29 @@ struct GroupBases {
   __device__ __forceinline__ void reach(const AttnArgs& a, const Span& sp, int h, int first, int last) {
     if (last >= g0 + kWave) fill(a, sp, h, first);
   }
-  __device__ __forceinline__ int64_t at(int g) const {
+  __device__ __forceinline__ uint64_t at(int g) const {
     const uint32_t x = __builtin_amdgcn_readlane(lo, g - g0), y = __builtin_amdgcn_readlane(hi, g - g0);
-    return (int64_t)((uint64_t)y << 32 | x);
+    return (uint64_t)y << 32 | x;
   }
 };
+// 16 bytes at a uniform address and a lane's offset
+__device__ __forceinline__ u4 load_at(uint64_t address, uint32_t offset) {
+  return *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(address) + offset);
+}
+// from an address in the K pool to the same row's in the V pool
+__device__ __forceinline__ uint64_t to_v(const PageView& c) {
+  return reinterpret_cast<uint64_t>(c.v) - reinterpret_cast<uint64_t>(c.k);
+}
+
+// f(0) .. f(N - 1), the number a constant in each
+template <int... I, typename F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(std::make_integer_sequence<int, N>(), f);
+}
 
 // x, for code that only some iterations run: what is computed from it is computed there, and
 // takes no register in the others
@@ -109,33 +143,35 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
+// the lane's number, computed anew: no register holds it from one use to the next
+__device__ __forceinline__ int lane_here() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
+  return x;
+}
+
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One output row (d values from d0 on, 4 of them): the result, or a range's partial.
-template <typename T, int D>
-__device__ __forceinline__ void store4(const AttnArgs& a, int split, int t, int hq, int d0, const float (&o)[4]) {
-  if (a.n_split > 1) {
-    *reinterpret_cast<float4*>(a.part_o + (((int64_t)split * a.T + t) * a.HG + hq) * D + d0) =
-        make_float4(o[0], o[1], o[2], o[3]);
+// Four outputs of a row from d0 on: the result, or (part: the row's place) a partial.
+template <typename T>
+__device__ __forceinline__ void store4(const AttnArgs& a, float* part, int64_t at, const float (&o)[4]) {
+  if (part) {
+    *reinterpret_cast<float4*>(part) = make_float4(o[0], o[1], o[2], o[3]);
   } else if constexpr (std::is_same<T, float>::value) {
-    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + ((int64_t)t * a.HG + hq) * D + d0) =
-        make_float4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(o[0], o[1], o[2], o[3]);
   } else {
     ushort4 w;
     w.x = f32_to_bf16_bits(o[0]);
     w.y = f32_to_bf16_bits(o[1]);
     w.z = f32_to_bf16_bits(o[2]);
     w.w = f32_to_bf16_bits(o[3]);
-    *reinterpret_cast<ushort4*>(static_cast<uint16_t*>(a.out) + ((int64_t)t * a.HG + hq) * D + d0) = w;
+    *reinterpret_cast<ushort4*>(static_cast<uint16_t*>(a.out) + at) = w;
   }
 }
 // its maximum (in scaled log2 units) and sum
-__device__ __forceinline__ void store_ml(const AttnArgs& a, int split, int t, int hq, float m, float l) {
-  if (a.n_split > 1) {
-    *reinterpret_cast<float2*>(a.part_ml + (((int64_t)split * a.T + t) * a.HG + hq) * 2) = make_float2(m, l);
-  } else if (a.lse) {
-    a.lse[(int64_t)t * a.HG + hq] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-  }
+__device__ __forceinline__ void store_ml(const AttnArgs& a, float* part, int64_t row, float m, float l) {
+  if (part) *reinterpret_cast<float2*>(part) = make_float2(m, l);
+  else if (a.lse) a.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -214,45 +250,151 @@ struct Tile {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(kBlock, 2) void page_tile_kernel(AttnArgs a) {
+// A row tile's key tiles: 0 of a number that no rows have, 1 at least otherwise.
+template <int BN, int R>
+__device__ __forceinline__ int key_tiles(const AttnArgs& a, int tile) {
+  int lo = 0, hi = a.c.S;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (first_tile<R>(a, mid) <= tile) lo = mid;
+    else hi = mid;
+  }
+  const Span sp(a, lo);
+  const int rows = sp.n * a.G, r0 = (tile - first_tile<R>(a, lo)) * R;
+  if (r0 >= rows) return 0;
+  return max((sp.sees(a, (min(r0 + R, rows) - 1) / a.G) + BN - 1) / BN, 1);
+}
+
+// Shares: the (head, row tile, key tile) triples in that order, cut into equal parts for at most
+// a.shares workgroups and none below kLeastShare triples.  What a workgroup cannot
+// finish of a row tile (its first and last at most) it leaves as a partial.
+constexpr int kMaxTiles = 1023;    // row tiles whose sums a workgroup keeps
+constexpr int kLeastShare = 4;
+struct Shares {
+  int64_t total;   // triples
+  int n;           // parts
+  __device__ __forceinline__ Shares(const AttnArgs& a, int per_head) : total((int64_t)per_head * a.c.H) {
+    n = (int)min((int64_t)a.shares, max(total / kLeastShare, (int64_t)1));
+  }
+  __device__ __forceinline__ int64_t begin(int i) const { return total * i / n; }
+  // the part that triple x is in
+  __device__ __forceinline__ int of(int64_t x) const { return (int)((x * n + n - 1) / total); }
+};
+
+// The sums of the row tiles' key tiles into s_sum (those before tile x at x), and this
+// workgroup's triples; false: it has none.
+template <int BN, int R>
+__device__ __forceinline__ bool share_out(const AttnArgs& a, uint32_t id, int* s_sum, int* s_wave,
+                                          int64_t& next, int64_t& end) {
+  constexpr int E = (kMaxTiles + 1) / kBlock;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int mine[E], sum = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int x = threadIdx.x * E + e;
+    mine[e] = sum;
+    if (x < a.n_tile) sum += key_tiles<BN, R>(a, x);
+  }
+  int upto = sum;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int z = __shfl_up(upto, o, kWave);
+    if (lane >= o) upto += z;
+  }
+  if (lane == kWave - 1) s_wave[wave] = upto;
+  __syncthreads();
+  int before = upto - sum;
+  for (int w = 0; w < wave; ++w) before += s_wave[w];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_sum[threadIdx.x * E + e] = before + mine[e];
+  __syncthreads();
+  if (id == 0)
+    for (int x = threadIdx.x; x <= a.n_tile; x += kBlock) a.sums[x] = s_sum[x];
+  const Shares sh(a, s_sum[a.n_tile]);
+  if (sh.total == 0 || (int)id >= sh.n) return false;
+  next = sh.begin(id);
+  end = sh.begin(id + 1);
+  return true;
+}
+
+// The key tiles [kt0, kt1) of a row tile and head; whole: all that there are.
+struct Segment {
+  int tile, h, kt0, kt1;
+  bool whole;
+};
+__device__ __forceinline__ Segment next_segment(const AttnArgs& a, const int* s_sum, int64_t& next, int64_t end) {
+  Segment g;
+  const int per_head = s_sum[a.n_tile];
+  g.h = (int)(next / per_head);
+  const int at = (int)(next - (int64_t)g.h * per_head);
+  int lo = 0, hi = a.n_tile;     // the last tile that begins at or before it, and is not empty
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (s_sum[mid] <= at) lo = mid;
+    else hi = mid;
+  }
+  g.tile = __builtin_amdgcn_readfirstlane(lo);
+  g.kt0 = at - s_sum[g.tile];
+  const int all = s_sum[g.tile + 1] - s_sum[g.tile];
+  g.kt1 = (int)min((int64_t)all, g.kt0 + (end - next));
+  g.whole = g.kt0 == 0 && g.kt1 == all;
+  next += g.kt1 - g.kt0;
+  return g;
+}
+
+// Workgroups that a CU holds (waves per SIMD).  fp32 rows of 128 take more than half of the
+// registers, Q alone 64, and their MFMAs, 8 times as long as bf16's, need no second wave.
+constexpr int tile_waves(bool bf16, int d) { return (d == 64 ? 2 : 1) + bf16; }
+
+template <typename T, int D, bool SHARES>
+__global__ __launch_bounds__(kBlock, tile_waves(std::is_same<T, bf16_t>::value, D)) void page_tile_kernel(AttnArgs a) {
   using S = Tile<T, D>;
   constexpr int BN = S::BN, NS = S::NS, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
   __shared__ u4 s_k[2][S::kPieces], s_v[2][S::kPieces];
   __shared__ int s_bad[D];
+  __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
+  __shared__ int s_wave[kWaves];
 
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, half = lane / 32;
-  // workgroups of one head and range side by side, on one XCD: they share its K and V
+  // workgroups of one head side by side, on one XCD: they share its K and V
   const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int tile = a.n_tile - 1 - (int)(id % a.n_tile);
-  const int h = (int)(id / a.n_tile) % a.c.H, split = (int)(id / a.n_tile) / a.c.H;
+  int64_t next = 0, end = 1;    // of this workgroup's triples
+  if constexpr (SHARES) {
+    if (!share_out<BN, kTileRows>(a, id, s_sum, s_wave, next, end)) return;
+  }
 
-  // tiles of slot s begin at number floor(cu[s] G / 128) + s: room for all of its rows
-  auto first_tile = [&](int s) { return (int)((int64_t)min(max(a.cu[s], 0), a.T) * a.G / kTileRows) + s; };
-  const Span sp(a, find_slot(a.c.S, tile, first_tile));
-  const int rows = sp.n * a.G, r0 = (tile - first_tile(sp.s)) * kTileRows;
-  if (r0 >= rows || rows <= a.split_rows) return;
+  for (int seg = 0; next < end; ++seg) {
+  Segment sg;
+  if constexpr (SHARES) {
+    sg = next_segment(a, s_sum, next, end);
+    if (seg) __syncthreads();      // the tile before is done with s_bad
+  } else {
+    sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};   // long ones first
+    next = end;
+  }
+  const int tile = sg.tile, h = sg.h;
+  const bool whole = sg.whole;
+  const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, s); }));
+  const int rows = sp.n * a.G, r0 = (tile - first_tile<kTileRows>(a, sp.s)) * kTileRows;
+  if (r0 >= rows) return;
 
-  // this lane's row, and the keys that it sees
-  const int row = min(r0 + 32 * wave + l32, rows - 1);
-  const int tok = row / a.G, g = row - tok * a.G;
-  const int lim = sp.sees(a, tok);
+  // the keys that this lane's row sees
+  const int lim = sp.sees(a, min(r0 + 32 * wave + l32, rows - 1) / a.G);
   const int wave_lo = __builtin_amdgcn_readfirstlane(lim);              // the wave's first row's
   const int wave_hi = __builtin_amdgcn_readlane(lim, 31);               // and its last row's
   const bool has_rows = r0 + 32 * wave < rows;
-  const int kb = split * a.keys;
-  int ke = sp.sees(a, (min(r0 + kTileRows, rows) - 1) / a.G);
-  if (split < a.n_split - 1) ke = min(ke, kb + a.keys);
-  if (kb >= ke && a.n_split > 1) return;   // combine takes no partial of this range
+  const int kb = sg.kt0 * BN;
+  const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kTileRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
   const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
   if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
   __syncthreads();
 
   u4 qf[KS];
   {
-    const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + g) * PPR + half;
+    const int row = min(r0 + 32 * wave + l32, rows - 1), tok = row / a.G;
+    const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = qp[2 * ks];
   }
@@ -265,17 +407,16 @@ __global__ __launch_bounds__(kBlock, 2) void page_tile_kernel(AttnArgs a) {
 
   GroupBases<PPR> bases;
   u4 rk[NP], rv[NP];
-  auto load = [&](int j0, const uint4* pool, u4 (&to)[NP]) {
+  auto load = [&](int j0, uint64_t pool, u4 (&to)[NP]) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int r = (i * kBlock + wave * kWave) / PPR;    // the wave's first row of this load
-      to[i] = reinterpret_cast<const u4*>(pool)[bases.at((j0 + r) / 16) +
-                                                ((i * kBlock + wave * kWave) % (16 * PPR) + lane)];
+      const int x = i * kBlock + wave * kWave;    // the wave's first piece of this load
+      to[i] = load_at(bases.at(j0 / 16 + x / (16 * PPR)) + pool, (x % (16 * PPR) + lane) * 16);
     }
   };
   auto stage = [&](int b, int j0) {
     if (j0 + BN > least) {
-      const int tid = here(threadIdx.x);
+      const int tid = wave * kWave + lane_here();
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int x = i * kBlock + tid, key = j0 + x / PPR;
@@ -293,19 +434,18 @@ __global__ __launch_bounds__(kBlock, 2) void page_tile_kernel(AttnArgs a) {
 
   if (kb < ke) {
     bases.fill(a, sp, h, kb / 16);
-    load(kb, a.c.k, rk);
-    load(kb, a.c.v, rv);
+    load(kb, 0, rk);
+    load(kb, to_v(a.c), rv);
     stage(0, kb);
   }
   int buf = 0;
   for (int j0 = kb; j0 < ke; j0 += BN, buf ^= 1) {
     __syncthreads();
     const bool more = j0 + BN < ke;
-    // fp32: V rows only behind the scores, whose operands take twice the registers
     if (more) {
       bases.reach(a, sp, h, (j0 + BN) / 16, (j0 + BN) / 16 + BN / 16 - 1);
-      load(j0 + BN, a.c.k, rk);
-      if (S::kBf16) load(j0 + BN, a.c.v, rv);
+      load(j0 + BN, 0, rk);
+      load(j0 + BN, to_v(a.c), rv);
     }
     if (has_rows && j0 < wave_hi) {
       const u4* tk = s_k[buf];
@@ -402,33 +542,455 @@ __global__ __launch_bounds__(kBlock, 2) void page_tile_kernel(AttnArgs a) {
         }
       }
     }
-    if (more) {
-      if (!S::kBf16) load(j0 + BN, a.c.v, rv);
-      stage(buf ^ 1, j0 + BN);
-    }
+    if (more) stage(buf ^ 1, j0 + BN);
   }
 
   __syncthreads();   // s_bad
-  if (!has_rows || r0 + 32 * wave + l32 >= rows) return;
-  l += __shfl_xor(l, 32, kWave);
-  const int t = sp.c0 + tok, hq = h * a.G + g;
-  const float mul = a.n_split > 1 ? 1.f : l > 0.f ? 1.f / l : l;   // no key: 0; NaN stays
-  if (half == 0) store_ml(a, split, t, hq, m * a.scale_log2, l);
+  if (has_rows) {
+    l += __shfl_xor(l, 32, kWave);
+    const int lane = lane_here(), half = lane / 32, r = 32 * wave + lane % 32;
+    const int row = r0 + r, tok = row / a.G;
+    const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;
+    // a partial's place: a workgroup's first row tile, or its last
+    const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kTileRows + r;
+    const float mul = !whole ? 1.f : l > 0.f ? 1.f / l : l;   // no key: 0; NaN stays
+    if (half == 0 && row < rows) store_ml(a, whole ? nullptr : a.part_ml + slot * 2, at, m * a.scale_log2, l);
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d0 = 32 * b + 8 * i + 4 * half;
-      float x[4];
+      for (int i = 0; i < 4 && row < rows; ++i) {
+        const int d0 = 32 * b + 8 * i + 4 * half;
+        float x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim ? __builtin_nanf("") : o[b][4 * i + e] * mul;
-      store4<T, D>(a, split, t, hq, d0, x);
-    }
+        for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim ? __builtin_nanf("") : o[b][4 * i + e] * mul;
+        store4<T>(a, whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
+      }
+  }
+  }
 }
 
 // ---------------------------------------------------------------------------
-// The few-row kernel: a workgroup takes one (range, head, slot), its waves every fourth tile
-// of 32 keys (fp32: 16).  K rows go from memory into A operands as they are, V rows
+// The wide tile kernel (bf16).  A wave keeps 64 query rows (two to a lane), so that every K and
+// V operand read from LDS feeds two MFMAs: with 32 rows LDS was as busy as the MFMAs.  MFMAs
+// and the softmax's VALU work hardly overlap between waves of a SIMD on this part, but
+// they do within one, so a wave has its SIMD to itself and its steps of 32 keys overlap:
+// step t's exponentials run beside the scores of step t + 1 and the V product of step t - 1.
+// Maxima that grow by less than 2^8 leave the reference alone (a probability is then at most
+// 2^8, its rounding to bf16 relative as before).
+// ---------------------------------------------------------------------------
+constexpr int kWideRows = 64 * kWaves;
+
+template <int D, bool SHARES>
+__global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
+  using S = Tile<bf16_t, D>;
+  constexpr int BN = S::BN, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
+  static_assert(BN == 64, "two steps of 32 keys");
+  __shared__ u4 s_k[3][S::kPieces], s_v[3][S::kPieces];
+  __shared__ int s_bad[D];
+  __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
+  __shared__ int s_wave[kWaves];
+
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l32 = lane % 32, half = lane / 32;
+  const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
+  int64_t next = 0, end = 1;
+  if constexpr (SHARES) {
+    if (!share_out<BN, kWideRows>(a, id, s_sum, s_wave, next, end)) return;
+  }
+
+  for (int seg = 0; next < end; ++seg) {
+  Segment sg;
+  if constexpr (SHARES) {
+    sg = next_segment(a, s_sum, next, end);
+    if (seg) __syncthreads();      // the tile before is done with LDS
+  } else {
+    sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};
+    next = end;
+  }
+  const int h = sg.h;
+  const Span sp(a, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, s); }));
+  const int rows = sp.n * a.G, r0 = (sg.tile - first_tile<kWideRows>(a, sp.s)) * kWideRows;
+  if (r0 >= rows) return;
+
+  // the keys that this lane's two rows see
+  int lim[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) lim[c] = sp.sees(a, min(r0 + 64 * wave + 32 * c + l32, rows - 1) / a.G);
+  const int wave_lo = __builtin_amdgcn_readfirstlane(lim[0]);           // the wave's first row's
+  const int kb = sg.kt0 * BN;
+  const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kWideRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
+  const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
+  const int steps = max((ke - kb + BN - 1) / BN, 0) * 2;   // whole tiles: what lies behind is masked
+  if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+  __syncthreads();
+
+  u4 qf[2][KS];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = min(r0 + 64 * wave + 32 * c + l32, rows - 1), tok = row / a.G;
+    const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = qp[2 * ks];
+      asm volatile("" : "+a"(qf[c][ks]));
+    }
+  }
+  pf32x16 o[NB][2];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][c][i] = 0.f;
+  // a row's reference m (in score units), mc (in log2 units), what a score must pass for m to
+  // follow, and the sum l over this lane's keys
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, alpha[2] = {1.f, 1.f};
+  float mc[2] = {0.f, 0.f}, pass[2] = {-INFINITY, -INFINITY};
+  bool grown = false;   // m has changed for the step in hand: O follows behind its V product
+
+  GroupBases<PPR> bases;
+  constexpr int kGroups = BN / 16;
+  u4 rk[NP], rv[NP];
+  uint64_t at_k[NP], at_v[NP];   // a tile's addresses: K's loads find them, V's follow a tile later
+  const uint64_t kv = to_v(a.c);
+  const uint32_t offset = (wave * kWave % (16 * PPR) + lane) * 16;
+  auto reach = [&](int j0) INLINE { bases.reach(a, sp, h, j0 / 16, j0 / 16 + kGroups - 1); };
+  auto load_k = [&](int j0, int i) INLINE {   // behind reach()
+    at_v[i] = at_k[i] + kv;
+    at_k[i] = bases.at(j0 / 16 + (i * kBlock + wave * kWave) / (16 * PPR));
+    rk[i] = load_at(at_k[i], offset);
+  };
+  auto load_v = [&](int i) INLINE { rv[i] = load_at(at_v[i], offset); };
+  auto put_k = [&](int b, int i) INLINE {
+    const int x = i * kBlock + threadIdx.x;
+    s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
+  };
+  auto put_v = [&](int b, int i) INLINE {
+    const int x = i * kBlock + threadIdx.x;
+    s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
+  };
+  auto clean_v = [&](int j0) INLINE {
+    if (j0 + BN > least) {
+      const int tid = wave * kWave + lane_here();
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int x = i * kBlock + tid, key = j0 + x / PPR;
+        rv[i] = key < sp.L ? rv[i] : u4{0, 0, 0, 0};
+        scrub<bf16_t>(rv[i], key, x % PPR * (D / PPR), s_bad);
+      }
+    }
+  };
+  // V^T operand of keys 32 x + 16 kk on, outputs 32 b on
+  const int kr = 4 * half + lane % 16 / 4, pc = 2 * (lane / 16 % 2) + lane % 4 / 2, by = lane % 2 * 8;
+  auto vt = [&](const u4* tv, int x, int kk, int b) INLINE {
+    return read_vt(tv, S::v_at(32 * x + 16 * kk + kr, 4 * b + pc) * 16 + by,
+                   S::v_at(32 * x + 16 * kk + 8 + kr, 4 * b + pc) * 16 + by);
+  };
+  // O stays in AGPRs, which leaves the other registers to what the VALU works on.  The compiler
+  // does not see these as MFMAs: o_ready() keeps O's readers behind them.
+  auto add_product = [&](const pbf16x8& v, const pbf16x8& p, pf32x16& x) INLINE {
+    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(p));
+  };
+  auto o_ready = [&]() INLINE {   // 32 wait states (19 needed behind the last MFMA)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(o[b][0]), "+a"(o[b][1]));
+  };
+  float top[2] = {0.f, 0.f};
+  u4 kf[KS];   // K operands of the next step
+  auto k_operand = [&](const u4* tk, int x, int ks) INLINE { kf[ks] = tk[S::k_at(32 * x + l32, 2 * ks + half)]; };
+  // One step: scores of the next 32 keys (kf) into `next`, the probabilities of the scores in
+  // `cur` (pn), the V product of those before (pp), and the K operands of the step after it
+  // (rows 32 kx on of tk).  Written out MFMA by MFMA, with what fits beside each: an MFMA takes
+  // the pipe for 32 cycles, in which the wave can issue 7 other instructions.  A lane's element
+  // goes through three of these places (argument, exponential, rounding), so that none of its
+  // parts waits for the one before.  Probabilities are rounded to bf16 (to nearest, 2^-8 of each
+  // at most); their sum is taken before, in fp32.
+  auto step = [&](const u4* tk, int kx, const u4* tv, int vx, pf32x16 (&cur)[2], pf32x16 (&next)[2],
+                  const u4 (&pp)[2][2], u4 (&pn)[2][2], auto beside) INLINE {
+    constexpr int Q = 2 * KS, V = 4 * NB, E = 32;      // MFMAs of each kind, elements of a lane
+    constexpr int per = E / (Q + V);                   // elements beside an MFMA
+    pbf16x8 vf[2][NB];
+    auto part0 = [&](auto e) INLINE {
+      if constexpr (e < E) cur[e / 16][e % 16] = __builtin_fmaf(cur[e / 16][e % 16], a.scale_log2, -mc[e / 16]);
+    };
+    auto part1 = [&](auto e) INLINE {
+      if constexpr (e < E) cur[e / 16][e % 16] = exp2_(cur[e / 16][e % 16]);
+    };
+    auto part2 = [&](auto e) INLINE {
+      constexpr int c = e / 16, i = e % 16;
+      l[c] += cur[c][i];
+      asm volatile("" : "+v"(l[c]));   // here, not behind the step
+      if constexpr (i % 2 == 1) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const pbf16x2 y = __builtin_convertvector(f2{cur[c][i - 1], cur[c][i]}, pbf16x2);
+        pn[i / 8][c][i % 8 / 2] = __builtin_bit_cast(uint32_t, y);
+      }
+    };
+    auto elements = [&](auto n) INLINE {
+      each<per>([&](auto y) INLINE {
+        part2(std::integral_constant<int, per * n + y>());
+        part1(std::integral_constant<int, per * n + y + per>());
+        part0(std::integral_constant<int, per * n + y + 2 * per>());
+      });
+    };
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) next[c][i] = 0.f;
+    each<2 * per>([&](auto e) INLINE { part0(e); });
+    each<per>([&](auto e) INLINE { part1(e); });
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the K operands, all in one wait
+    __builtin_amdgcn_sched_barrier(0);
+    each<Q>([&](auto n) INLINE {
+      constexpr int ks = n / 2, c = n % 2, x = n - Q / 2;
+      next[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
+                                                        __builtin_bit_cast(pbf16x8, qf[c][ks]), next[c], 0, 0, 0);
+      if constexpr (x >= 0 && x < 2 * NB) vf[x / NB][x % NB] = vt(tv, vx, x / NB, x % NB);
+      if constexpr (x < 0) beside(n);
+      elements(n);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    each<V>([&](auto n) INLINE {
+      constexpr int kk = n / (2 * NB), b = n / 2 % NB, c = n % 2;
+      add_product(vf[kk][b], __builtin_bit_cast(pbf16x8, pp[kk][c]), o[b][c]);
+      if constexpr (n % 2 == 0 && n / 2 < KS) k_operand(tk, kx, n / 2);
+      elements(std::integral_constant<int, Q + decltype(n)::value>());
+      // the highest of the next scores, from behind their last MFMA on
+      if constexpr (n >= 2) {
+        constexpr int most = ((E + V - 3) / (V - 2) + 1) / 2 * 2;
+        constexpr int e0 = (n - 2) * most, e1 = (n - 1) * most < E ? (n - 1) * most : E;
+        each<(e1 > e0 ? e1 - e0 : 0)>([&](auto y) INLINE {
+          constexpr int e = e0 + y;
+          top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], next[e / 16][e % 16]) : next[e / 16][0];
+        });
+        asm volatile("" : "+v"(top[0]), "+v"(top[1]));   // here, not behind the step
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) asm volatile("" : "+v"(pn[kk][c]));
+  };
+  // a step's scores masked, and its reference: keys from j on
+  auto settle = [&](pf32x16 (&s)[2], int j, bool first = false) INLINE {
+    if (first || j + 32 > min(wave_lo, ke)) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int left = min(here(lim[c]), ke) - j - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[c][i] = 8 * (i / 4) + i % 4 < left ? s[c][i] : -INFINITY;
+        top[c] = s[c][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[c] = __builtin_elementwise_maximum(top[c], s[c][i]);
+      }
+    }
+    grown = __ballot(top[0] > pass[0] || top[1] > pass[1]) != 0;
+    if (grown) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float now = fmaxf(m[c], fmaxf(top[c], __shfl_xor(top[c], 32, kWave)));
+        alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
+        m[c] = now;
+        mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
+        pass[c] = now + 8.f / a.scale_log2;
+        l[c] *= alpha[c];
+      }
+    }
+  };
+  auto follow = [&]() INLINE {
+    if (grown) {
+      o_ready();
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[b][c][i] *= alpha[c];
+          asm volatile("s_nop 7" : "+a"(o[b][c]));
+        }
+    }
+  };
+
+  if (steps > 0) {
+    bases.fill(a, sp, h, kb / 16);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) at_k[i] = 0;
+    auto load_tile = [&](int j0) INLINE {
+      reach(j0);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) load_k(j0, i);
+    };
+    load_tile(kb);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) rv[i] = load_at(at_k[i] + kv, offset);
+    clean_v(kb);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      put_k(0, i);
+      put_v(0, i);
+      put_v(2, i);                // for step 0's product, with probabilities of 0
+    }
+    load_tile(kb + BN);           // behind the last key: the last group again
+#pragma unroll
+    for (int i = 0; i < NP; ++i) put_k(1, i);
+    load_tile(kb + 2 * BN);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) load_v(i);
+    __syncthreads();
+    pf32x16 s0[2], s1[2];
+    u4 p0[2][2], p1[2][2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) p1[kk][c] = u4{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 0, ks);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s0[c][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        s0[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
+                                                        __builtin_bit_cast(pbf16x8, qf[c][ks]), s0[c], 0, 0, 0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 1, ks);
+    settle(s0, kb, true);
+    // 64 keys.  Of K, tile b and the next are read and the one behind it written; of V, the
+    // tile before, tile b, and the next: three buffers of each, one barrier.
+    auto stage = [&](auto buffer, int j0) INLINE {
+      constexpr int b = decltype(buffer)::value, b1 = (b + 1) % 3, b2 = (b + 2) % 3;
+      __syncthreads();
+      // a tile's loads right behind the stores of the one before: nearly two steps ahead
+      reach(j0 + 3 * BN);
+      step(s_k[b1], 0, s_v[b2], 1, s0, s1, p1, p0, [&](auto n) INLINE {
+        if constexpr (n < NP) put_k(b2, n);
+        else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
+      });
+      follow();
+      settle(s1, j0 + 32);
+      clean_v(j0 + BN);
+      step(s_k[b1], 1, s_v[b], 0, s1, s0, p0, p1, [&](auto n) INLINE {
+        if constexpr (n < NP) put_v(b1, n);
+        else if constexpr (n < 2 * NP) load_v(n - NP);
+      });
+      follow();
+      settle(s0, j0 + 64);
+    };
+    for (int t = 0; t < steps; t += 6) {
+      stage(std::integral_constant<int, 0>(), kb + 32 * t);
+      if (t + 2 >= steps) break;
+      stage(std::integral_constant<int, 1>(), kb + 32 * t + 64);
+      if (t + 4 >= steps) break;
+      stage(std::integral_constant<int, 2>(), kb + 32 * t + 128);
+    }
+    const u4* tv = s_v[(steps / 2 - 1) % 3];   // the last step's product
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const pbf16x8 w = vt(tv, 1, kk, b);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) add_product(w, __builtin_bit_cast(pbf16x8, p1[kk][c]), o[b][c]);
+      }
+    o_ready();
+  }
+
+  __syncthreads();   // s_bad
+  {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      l[c] += __shfl_xor(l[c], 32, kWave);
+      const int lane = lane_here(), half = lane / 32, r = 64 * wave + 32 * c + lane % 32;
+      const int row = r0 + r, tok = row / a.G;
+      const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;
+      // a partial's place: a workgroup's first row tile, or its last
+      const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kWideRows + r;
+      const float mul = !sg.whole ? 1.f : l[c] > 0.f ? 1.f / l[c] : l[c];   // no key: 0; NaN stays
+      if (row < rows) {
+        if (half == 0) store_ml(a, sg.whole ? nullptr : a.part_ml + slot * 2, at, m[c] * a.scale_log2, l[c]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int d0 = 32 * b + 8 * i + 4 * half;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim[c] ? __builtin_nanf("") : o[b][c][4 * i + e] * mul;
+            store4<bf16_t>(a, sg.whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
+          }
+      }
+    }
+  }
+  }
+}
+
+// Behind shares: the rows of each (row tile, head) joined in the order of the keys, if several
+// shares have some of them.  A thread takes 4 outputs of one row, so that a call of few rows
+// still has many workgroups: it is a chain of memory latencies.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
+  constexpr int TPR = D / 4, RPB = kBlock / TPR, kPer = R / RPB;   // threads of a row, ...
+  constexpr int U = 4;                                                    // partials in flight
+  const int tile = (int)(blockIdx.x / kPer) % a.n_tile, h = (int)(blockIdx.x / kPer) / a.n_tile;
+  const int per_head = a.sums[a.n_tile], sum0 = a.sums[tile], sum1 = a.sums[tile + 1];
+  if (sum1 <= sum0) return;
+  const Shares sh(a, per_head);
+  const int64_t x0 = (int64_t)h * per_head + sum0, x1 = (int64_t)h * per_head + sum1;
+  const int first = sh.of(x0), last = sh.of(x1 - 1);
+  if (first == last) return;   // whole: already written
+  // the first part's partial is that of its last row tile if it began before this one; the others
+  // begin in it
+  const int64_t place0 = ((int64_t)first * 2 + (sh.begin(first) < x0)) * R;
+  const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<R>(a, s); }));
+  const int r0 = (tile - first_tile<R>(a, sp.s)) * R;
+  const int d0 = threadIdx.x % TPR * 4, r = (int)(blockIdx.x % kPer) * RPB + threadIdx.x / TPR;
+  if (r0 + r >= sp.n * a.G) return;
+  auto place = [&](int i) { return (i == first ? place0 : (int64_t)i * 2 * R) + r; };
+  auto ml = [&](int i) { return *reinterpret_cast<const float2*>(a.part_ml + place(i) * 2); };
+  float top = -INFINITY;
+  for (int i = first; i <= last; i += U) {
+    float m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = ml(min(i + u, last)).x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
+  }
+  float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = first; i <= last; i += U) {
+    float2 y[U];
+    float4 z[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      y[u] = ml(min(i + u, last));
+      z[u] = *reinterpret_cast<const float4*>(a.part_o + place(min(i + u, last)) * D + d0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u > last) break;
+      const float f = y[u].x == -INFINITY ? 0.f : exp2_(y[u].x - top);
+      l += y[u].y * f;
+      x[0] += z[u].x * f;
+      x[1] += z[u].y * f;
+      x[2] += z[u].z * f;
+      x[3] += z[u].w * f;
+    }
+  }
+  const float mul = l > 0.f ? 1.f / l : l;
+  const int tok = (r0 + r) / a.G;
+  const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + r0 + r - tok * a.G;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] *= mul;
+  store4<T>(a, nullptr, at * D + d0, x);
+  if (d0 == 0) store_ml(a, nullptr, at, top, l);
+}
+
+// ---------------------------------------------------------------------------
+// The few-row kernel: a workgroup takes one (range, head, row tile of 16), its waves every
+// fourth tile of 32 keys (fp32: 16).  K rows go from memory into A operands as they are, V rows
 // through a piece of LDS that the wave has alone; the waves' states are joined at the
 // end.  The next tile's rows are loaded as soon as this one's have left their registers.
 // ---------------------------------------------------------------------------
@@ -464,21 +1026,24 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   const int l16 = lane % 16, quad = lane / 16;
   const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
   const int split = (int)(id % a.n_split), h = (int)(id / a.n_split) % a.c.H;
-  const Span sp(a, (int)(id / a.n_split) / a.c.H);
-  const int rows = sp.n * a.G;
-  if (rows == 0) return;
-  if (rows > kFewRows) {
-    // the tile kernel's, unless max_new said that there is none of these
-    if (a.split_rows == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
+  const int tile = (int)(id / a.n_split) / a.c.H;
+  const Span sp(a, a.by_slot ? tile : find_slot(a.c.S, tile, [&](int s) { return first_tile<kFewRows>(a, s); }));
+  const int r0 = a.by_slot ? 0 : (tile - first_tile<kFewRows>(a, sp.s)) * kFewRows;
+  const int rows = min(sp.n * a.G - r0, kFewRows);   // of this tile
+  if (rows <= 0) return;
+  // more tokens than max_new said
+  if (a.by_slot && sp.n * a.G > kFewRows) {
+    if (threadIdx.x == 0 && a.status) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
     return;
   }
-  const int row = min(l16, rows - 1);
+  const int row = r0 + min(l16, rows - 1);
   const int tok = row / a.G, g = row - tok * a.G;
   const int lim = sp.sees(a, tok);
-  const int least = sp.sees(a, 0);
+  const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
   const int kb = split * a.keys;
-  const int ke = split < a.n_split - 1 ? min(sp.L, kb + a.keys) : sp.L;
-  if (kb >= ke && a.n_split > 1) return;
+  int ke = sp.sees(a, (r0 + rows - 1) / a.G);
+  if (split < a.n_split - 1) ke = min(ke, kb + a.keys);
+  if (kb >= ke && a.n_split > 1) return;   // combine takes no partial of this range
   if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
   __syncthreads();
 
@@ -499,13 +1064,11 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
     bases.reach(a, sp, h, j0 / 16, j0 / 16 + NS - 1);
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const int64_t at = bases.at(j0 / 16 + n);
-      const u4* kp = reinterpret_cast<const u4*>(a.c.k) + at + l16 * PPR + quad;
+      const uint64_t at = bases.at(j0 / 16 + n);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) rk[n][ks] = kp[4 * ks];
-      const u4* vp = reinterpret_cast<const u4*>(a.c.v) + at + lane;
+      for (int ks = 0; ks < KS; ++ks) rk[n][ks] = load_at(at, (l16 * PPR + 4 * ks + quad) * 16);
 #pragma unroll
-      for (int i = 0; i < NP / NS; ++i) rv[n * (NP / NS) + i] = vp[i * kWave];
+      for (int i = 0; i < NP / NS; ++i) rv[n * (NP / NS) + i] = load_at(at + to_v(a.c), (i * kWave + lane) * 16);
     }
   };
   u4* tv = s_v[wave];
@@ -516,7 +1079,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   }
   for (int j0 = j_first; j0 < ke; j0 += kWaves * BN) {
     if (j0 + BN > least) {
-      const int at = here(lane);
+      const int at = lane_here();
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int x = i * kWave + at, key = j0 + x / PPR;
@@ -630,17 +1193,21 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
       x[2] += y.z * f;
       x[3] += y.w * f;
     }
-    const int ti = r / a.G, t = sp.c0 + ti, hq = h * a.G + r - ti * a.G;
-    const float mul = a.n_split > 1 ? 1.f : ll > 0.f ? 1.f / ll : ll;
+    const int ti = (r0 + r) / a.G;
+    const int64_t at = (int64_t)(sp.c0 + ti) * a.HG + h * a.G + r0 + r - ti * a.G;
+    const int64_t part = (int64_t)split * a.T * a.HG + at;
+    const bool whole = a.n_split == 1;
+    const float mul = !whole ? 1.f : ll > 0.f ? 1.f / ll : ll;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = s_bad[d0 + i] < sp.sees(a, ti) ? __builtin_nanf("") : x[i] * mul;
-    store4<T, D>(a, split, t, hq, d0, x);
-    if (d0 == 0) store_ml(a, split, t, hq, mm * a.scale_log2, ll);
+    store4<T>(a, whole ? nullptr : a.part_o + part * D + d0, at * D + d0, x);
+    if (d0 == 0) store_ml(a, whole ? nullptr : a.part_ml + part * 2, at, mm * a.scale_log2, ll);
   }
 }
 
 // ---------------------------------------------------------------------------
-// A wave per (token, query head): the ranges that hold a key the token sees, joined in order.
+// Behind the few-row kernel's ranges: a wave per (token, query head), those that hold a key the
+// token sees joined in order.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
@@ -651,11 +1218,9 @@ __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
   if (t >= a.T || t >= a.cu[a.c.S]) return;
   const Span sp(a, find_slot(a.c.S, t, [&](int i) { return a.cu[i]; }));
   if (t < sp.c0 || t >= sp.c0 + sp.n) return;
-  const bool few = sp.n * a.G <= a.split_rows;
-  const int n_split = few ? a.few_split : a.n_split, keys = few ? a.few_keys : a.keys;
-  if (n_split == 1) return;   // already written
+  if (a.by_slot && sp.n * a.G > kFewRows) return;   // left out
   const int sees = sp.sees(a, t - sp.c0);
-  const int n = min(n_split, (sees + keys - 1) / keys);
+  const int n = min(a.n_split, (sees + a.keys - 1) / a.keys);
   const int64_t row = (int64_t)a.T * a.HG;     // rows of a range's partials
   float m = -INFINITY, l = 0.f;
   if (lane < n) {
@@ -685,59 +1250,69 @@ __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
 
 template <typename T, int D>
 hipError_t launch_td(AttnArgs a, const PageAttnPlan& pl, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.T * a.HG;
+  const dim3 each((unsigned)((rows + kWaves - 1) / kWaves)), block(kBlock);   // a wave to a row
   if (pl.few) {
-    AttnArgs f = a;
-    f.n_split = pl.split_f;
-    f.keys = pl.keys_f;
-    f.split_rows = pl.tile ? kFewRows : 0;
-    hipLaunchKernelGGL((page_few_kernel<T, D>), dim3((unsigned)(a.c.S * a.c.H * pl.split_f)), dim3(kBlock), 0,
-                       stream, f);
-  }
-  a.n_split = pl.split_t;
-  a.keys = pl.keys_t;
-  a.split_rows = pl.few ? kFewRows : 0;
-  if (pl.tile)
-    hipLaunchKernelGGL((page_tile_kernel<T, D>), dim3((unsigned)(pl.n_tile * a.c.H * pl.split_t)), dim3(kBlock), 0,
-                       stream, a);
-  if (pl.split_t > 1 || pl.split_f > 1) {
-    a.few_split = pl.split_f;
-    a.few_keys = pl.keys_f;
-    const int64_t n = (int64_t)a.T * a.HG;
-    hipLaunchKernelGGL((page_combine_kernel<T, D>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0,
-                       stream, a);
+    hipLaunchKernelGGL((page_few_kernel<T, D>), dim3((unsigned)(a.n_tile * a.c.H * a.n_split)), block, 0, stream, a);
+    if (a.n_split > 1) hipLaunchKernelGGL((page_combine_kernel<T, D>), each, block, 0, stream, a);
+  } else {
+    constexpr bool kWide = std::is_same<T, bf16_t>::value;
+    constexpr int R = kWide ? kWideRows : kTileRows;
+    const dim3 grid(pl.shares ? pl.shares : (unsigned)(a.n_tile * a.c.H));
+    if constexpr (kWide) {
+      if (pl.shares) hipLaunchKernelGGL((page_wide_kernel<D, true>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((page_wide_kernel<D, false>), grid, block, 0, stream, a);
+    } else {
+      if (pl.shares) hipLaunchKernelGGL((page_tile_kernel<T, D, true>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((page_tile_kernel<T, D, false>), grid, block, 0, stream, a);
+    }
+    if (pl.shares)
+      hipLaunchKernelGGL((page_join_kernel<T, D, R>), dim3((unsigned)(a.n_tile * a.c.H * (R * D / 4 / kBlock))), block,
+                         0, stream, a);
   }
   return hipGetLastError();
-}
-
-// ranges of a multiple of `unit` keys, about `want` of them but none below `least` keys
-void split_keys(int max_len, int64_t want, int least, int unit, int& n, int& keys) {
-  int64_t s = want < kMaxSplit ? want : kMaxSplit;
-  if (s > max_len / least) s = max_len / least;
-  if (s < 1) s = 1;
-  keys = (int)(((max_len + s - 1) / s + unit - 1) / unit * unit);
-  n = (max_len + keys - 1) / keys;
 }
 
 }  // namespace
 
 PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int max_len) {
-  PageAttnPlan p;
+  PageAttnPlan p{};
   const int slots = c.S < T ? c.S : T;      // that can have tokens
-  p.tile = (int64_t)max_new * G > kFewRows;
-  p.few = !p.tile || (slots > 1 && (int64_t)T * G < 64 * (int64_t)slots);
-  p.n_tile = (int)((int64_t)T * G / kTileRows) + c.S;
-  p.split_t = p.split_f = 1;
-  p.keys_t = p.keys_f = max_len;
-  // a range is worth its partials from about 512 keys (tile) or 256 (few) on
-  if (p.tile) {
-    const int64_t wgs = ((int64_t)T * G / kTileRows + 1) * c.H;
-    split_keys(max_len, 512 / wgs, 512, 64, p.split_t, p.keys_t);
-  }
-  if (p.few) split_keys(max_len, 2048 / ((int64_t)slots * c.H) + 1, 256, 128, p.split_f, p.keys_f);
-  const int n = p.split_t > p.split_f ? p.split_t : p.split_f;
   const size_t rows = (size_t)T * c.H * G;
-  p.off_ml = n > 1 ? (size_t)n * rows * c.d * sizeof(float) : 0;
-  p.bytes = n > 1 ? p.off_ml + (size_t)n * rows * 2 * sizeof(float) : 0;
+  p.by_slot = (int64_t)max_new * G <= kFewRows;
+  p.few = p.by_slot;
+  p.n_split = 1;
+  p.keys = max_len;
+  if (p.few) {
+    p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + c.S;
+    // at least 256 keys to a range, up to kMaxSplit ranges
+    const int64_t wgs = (p.by_slot ? slots : (int64_t)T * G / kFewRows + 1) * c.H;
+    int64_t s = 2048 / wgs + 1;
+    if (s > kMaxSplit) s = kMaxSplit;
+    if (s > max_len / 256) s = max_len / 256;
+    if (s < 1) s = 1;
+    p.keys = (int)(((max_len + s - 1) / s + 127) / 128 * 128);
+    p.n_split = (max_len + p.keys - 1) / p.keys;
+    if (p.n_split > 1) {
+      p.off_ml = p.n_split * rows * c.d * sizeof(float);
+      p.bytes = p.off_ml + p.n_split * rows * 2 * sizeof(float);
+    }
+    return p;
+  }
+  const bool wide = c.dtype == VASE_BF16;
+  const int R = wide ? kWideRows : kTileRows;
+  p.n_tile = (int)((int64_t)T * G / R) + c.S;
+  // Shared out below 640 row tiles.
+  // The sums of 32-key tiles stay in 32 bits.
+  const int64_t tiles = ((int64_t)T * G / R + 1) * c.H;
+  if (tiles < 640 && p.n_tile <= kMaxTiles && max_len > 1024 &&
+      (int64_t)p.n_tile * (c.M * c.page / 32 + 1) <= 0x7fffffff) {
+    p.shares = 256 * (wide ? 1 : tile_waves(false, c.d));
+    const size_t part = (size_t)p.shares * 2 * R;
+    p.off_ml = part * c.d * sizeof(float);
+    p.off_sums = p.off_ml + part * 2 * sizeof(float);
+    p.bytes = p.off_sums + (kMaxTiles + 1) * sizeof(int32_t);
+  }
   return p;
 }
 
@@ -756,8 +1331,13 @@ hipError_t launch_page_attn(const vase_pages& c, const void* q, int64_t q_stride
   a.out = out;
   a.lse = lse;
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = ws ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.off_ml) : nullptr;
+  a.part_ml = plan.bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.off_ml) : nullptr;
+  a.sums = plan.shares ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + plan.off_sums) : nullptr;
   a.n_tile = plan.n_tile;
+  a.n_split = plan.n_split;
+  a.keys = plan.keys;
+  a.by_slot = plan.by_slot;
+  a.shares = plan.shares;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c.d);
   a.status = status;
   if (c.dtype == VASE_BF16)

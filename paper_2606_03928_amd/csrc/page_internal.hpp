@@ -71,11 +71,12 @@ __device__ __forceinline__ int find_slot(int S, int t, F f) {
 
 // page_attn.hip
 struct PageAttnPlan {
-  bool tile, few;          // the launches: slots of many rows, slots of few
+  bool few;                // 16 rows to a workgroup; else 128
+  bool by_slot;            // few: max_new * G <= 16, a slot is one row tile
   int n_tile;              // row tiles of the batch, at most
-  int split_t, keys_t;     // key ranges of the tile kernel and their length
-  int split_f, keys_f;     // those of the few-row kernel
-  size_t off_ml, bytes;    // workspace: partial outputs, then their maxima and sums
+  int n_split, keys;       // few: key ranges and their length
+  int shares;              // else: workgroups among which the work is shared out, or 0
+  size_t off_ml, off_sums, bytes;   // workspace: partial outputs, their maxima and sums, ...
 };
 PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int max_len);
 hipError_t launch_page_attn(const vase_pages& c, const void* q, int64_t q_stride, const int32_t* cu,
