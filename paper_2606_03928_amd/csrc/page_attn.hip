@@ -28,6 +28,7 @@ namespace vase {
 namespace {
 
 typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 pbf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 pbf16x2 __attribute__((ext_vector_type(2)));
 typedef short ps16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short pu16x2 __attribute__((ext_vector_type(2)));
@@ -42,7 +43,7 @@ typedef __attribute__((address_space(3))) ps16x4 lds_s16x4;
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kTileRows = 32 * kWaves;   // query rows of a tile workgroup
-constexpr int kFewRows = 16;             // most query rows of a few-row workgroup
+constexpr int kFewRows = 16;             // query rows of a few-row workgroup
 constexpr int kMaxSplit = 64;
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -69,11 +70,12 @@ struct AttnArgs {
 // A slot's share of the batch, read as it stands but kept inside the caller's arrays.
 struct Span {
   int s, c0, n, L;   // slot, first token, tokens, rows
-  __device__ __forceinline__ Span(const AttnArgs& a, int slot) : s(slot) {
-    c0 = min(max(a.cu[s], 0), a.T);
-    n = min(max(a.cu[s + 1], c0), a.T) - c0;
+  __device__ __forceinline__ Span(const AttnArgs& a, const int32_t* cu, int slot) : s(slot) {
+    c0 = min(max(cu[s], 0), a.T);
+    n = min(max(cu[s + 1], c0), a.T) - c0;
     L = slot_len(a.c, s);
   }
+  __device__ __forceinline__ Span(const AttnArgs& a, int slot) : Span(a, a.cu, slot) {}
   // rows that token i sees
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {
     return a.causal ? max(L - n + i + 1, 0) : L;
@@ -83,8 +85,12 @@ struct Span {
 // Row tiles of R rows: those of slot s begin at number floor(cu[s] G / R) + s, which leaves
 // room for all of its rows, so that a tile's slot is found in cu alone.
 template <int R>
+__device__ __forceinline__ int first_tile(const AttnArgs& a, const int32_t* cu, int s) {
+  return (int)((int64_t)min(max(cu[s], 0), a.T) * a.G / R) + s;
+}
+template <int R>
 __device__ __forceinline__ int first_tile(const AttnArgs& a, int s) {
-  return (int)((int64_t)min(max(a.cu[s], 0), a.T) * a.G / R) + s;
+  return first_tile<R>(a, a.cu, s);
 }
 
 // Where the 16-row groups of a slot lie: lane l holds the address of group g0 + l of head h in
@@ -219,7 +225,6 @@ __device__ __forceinline__ pbf16x8 read_vt(const u4* base, int byte0, int byte1)
   const ps16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + byte1));
   return __builtin_bit_cast(pbf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-__device__ __forceinline__ pbf16x8 to_bf16x8(const pf32x8& x) { return __builtin_convertvector(x, pbf16x8); }
 
 // ---------------------------------------------------------------------------
 // The tile kernel.  A wave keeps 32 query rows (one per lane column) and their O^T in
@@ -230,7 +235,6 @@ template <typename T, int D>
 struct Tile {
   static constexpr bool kBf16 = std::is_same<T, bf16_t>::value;
   static constexpr int BN = kBf16 ? 64 : 32;          // keys
-  static constexpr int NS = BN / 32;                  // MFMA results of 32 keys
   static constexpr int PPR = D * (kBf16 ? 2 : 4) / 16;
   static constexpr int kPieces = BN * PPR;
   static constexpr int NP = kPieces / kBlock;         // of each, per thread
@@ -250,26 +254,13 @@ struct Tile {
   }
 };
 
-// A row tile's key tiles: 0 of a number that no rows have, 1 at least otherwise.
-template <int BN, int R>
-__device__ __forceinline__ int key_tiles(const AttnArgs& a, int tile) {
-  int lo = 0, hi = a.c.S;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (first_tile<R>(a, mid) <= tile) lo = mid;
-    else hi = mid;
-  }
-  const Span sp(a, lo);
-  const int rows = sp.n * a.G, r0 = (tile - first_tile<R>(a, lo)) * R;
-  if (r0 >= rows) return 0;
-  return max((sp.sees(a, (min(r0 + R, rows) - 1) / a.G) + BN - 1) / BN, 1);
-}
-
 // Shares: the (head, row tile, key tile) triples in that order, cut into equal parts for at most
-// a.shares workgroups and none below kLeastShare triples.  What a workgroup cannot
-// finish of a row tile (its first and last at most) it leaves as a partial.
+// a.shares workgroups and none below kLeastShare triples.  A row tile's beginning and end (Q, the
+// first loads, its output: 9 us) count as kSetup triples before its first.  What a workgroup
+// cannot finish of a row tile (its first and last at most) it leaves as a partial.
 constexpr int kMaxTiles = 1023;    // row tiles whose sums a workgroup keeps
 constexpr int kLeastShare = 4;
+constexpr int kSetup = 6;
 struct Shares {
   int64_t total;   // triples
   int n;           // parts
@@ -281,19 +272,42 @@ struct Shares {
   __device__ __forceinline__ int of(int64_t x) const { return (int)((x * n + n - 1) / total); }
 };
 
-// The sums of the row tiles' key tiles into s_sum (those before tile x at x), and this
-// workgroup's triples; false: it has none.
+// cu, of which a slot is searched for often: S < n_tile <= kMaxTiles
+__device__ __forceinline__ void keep_cu(const AttnArgs& a, int32_t* s_cu) {
+  for (int x = threadIdx.x; x <= a.c.S; x += kBlock) s_cu[x] = a.cu[x];
+}
+
+// A row tile's triples: 0 of a number that no rows have, otherwise one key tile at least.
 template <int BN, int R>
-__device__ __forceinline__ bool share_out(const AttnArgs& a, uint32_t id, int* s_sum, int* s_wave,
+__device__ __forceinline__ int key_tiles(const AttnArgs& a, const int32_t* s_cu, int tile) {
+  int lo = 0, hi = a.c.S;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (first_tile<R>(a, s_cu, mid) <= tile) lo = mid;
+    else hi = mid;
+  }
+  const Span sp(a, s_cu, lo);
+  const int rows = sp.n * a.G, r0 = (tile - first_tile<R>(a, s_cu, lo)) * R;
+  if (r0 < 0 || r0 >= rows) return 0;
+  return kSetup + max((sp.sees(a, (min(r0 + R, rows) - 1) / a.G) + BN - 1) / BN, 1);
+}
+
+// cu into s_cu, the sums of the row tiles' triples into s_sum (those before tile x at x), and
+// this workgroup's triples; false: it has none.
+template <int BN, int R>
+__device__ __forceinline__ bool share_out(const AttnArgs& a, uint32_t id, int32_t* s_cu, int* s_sum, int* s_wave,
                                           int64_t& next, int64_t& end) {
   constexpr int E = (kMaxTiles + 1) / kBlock;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  keep_cu(a, s_cu);
+  __syncthreads();
+  for (int x = threadIdx.x; x <= kMaxTiles; x += kBlock) s_sum[x] = x < a.n_tile ? key_tiles<BN, R>(a, s_cu, x) : 0;
+  __syncthreads();
   int mine[E], sum = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int x = threadIdx.x * E + e;
     mine[e] = sum;
-    if (x < a.n_tile) sum += key_tiles<BN, R>(a, x);
+    sum += s_sum[threadIdx.x * E + e];
   }
   int upto = sum;
 #pragma unroll
@@ -334,25 +348,28 @@ __device__ __forceinline__ Segment next_segment(const AttnArgs& a, const int* s_
     else hi = mid;
   }
   g.tile = __builtin_amdgcn_readfirstlane(lo);
-  g.kt0 = at - s_sum[g.tile];
-  const int all = s_sum[g.tile + 1] - s_sum[g.tile];
-  g.kt1 = (int)min((int64_t)all, g.kt0 + (end - next));
-  g.whole = g.kt0 == 0 && g.kt1 == all;
-  next += g.kt1 - g.kt0;
+  const int first = at - s_sum[g.tile], all = s_sum[g.tile + 1] - s_sum[g.tile];
+  const int upto = (int)min((int64_t)all, first + (end - next));
+  g.kt0 = max(first - kSetup, 0);
+  g.kt1 = max(upto - kSetup, 0);   // none: another workgroup's
+  g.whole = g.kt0 == 0 && upto == all;
+  next += upto - first;
   return g;
 }
 
-// Workgroups that a CU holds (waves per SIMD).  fp32 rows of 128 take more than half of the
-// registers, Q alone 64, and their MFMAs, 8 times as long as bf16's, need no second wave.
-constexpr int tile_waves(bool bf16, int d) { return (d == 64 ? 2 : 1) + bf16; }
+// Workgroups that a CU holds (waves per SIMD).  Rows of 128 take more than half of the registers,
+// Q alone 64, and fp32 MFMAs, 8 times as long as bf16's, need no second wave.
+constexpr int tile_waves(int d) { return d == 64 ? 2 : 1; }
 
-template <typename T, int D, bool SHARES>
-__global__ __launch_bounds__(kBlock, tile_waves(std::is_same<T, bf16_t>::value, D)) void page_tile_kernel(AttnArgs a) {
-  using S = Tile<T, D>;
-  constexpr int BN = S::BN, NS = S::NS, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
+template <int D, bool SHARES>
+__global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnArgs a) {
+  using S = Tile<float, D>;
+  constexpr int BN = S::BN, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
+  static_assert(BN == 32, "one MFMA result of keys");
   __shared__ u4 s_k[2][S::kPieces], s_v[2][S::kPieces];
   __shared__ int s_bad[D];
   __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
+  __shared__ int32_t s_cu[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int s_wave[kWaves];
 
   const int lane = threadIdx.x % kWave;
@@ -360,212 +377,169 @@ __global__ __launch_bounds__(kBlock, tile_waves(std::is_same<T, bf16_t>::value, 
   const int l32 = lane % 32, half = lane / 32;
   // workgroups of one head side by side, on one XCD: they share its K and V
   const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int32_t* cu = SHARES ? s_cu : a.cu;
   int64_t next = 0, end = 1;    // of this workgroup's triples
   if constexpr (SHARES) {
-    if (!share_out<BN, kTileRows>(a, id, s_sum, s_wave, next, end)) return;
+    if (!share_out<BN, kTileRows>(a, id, s_cu, s_sum, s_wave, next, end)) return;
   }
 
   for (int seg = 0; next < end; ++seg) {
-  Segment sg;
-  if constexpr (SHARES) {
-    sg = next_segment(a, s_sum, next, end);
-    if (seg) __syncthreads();      // the tile before is done with s_bad
-  } else {
-    sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};   // long ones first
-    next = end;
-  }
-  const int tile = sg.tile, h = sg.h;
-  const bool whole = sg.whole;
-  const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, s); }));
-  const int rows = sp.n * a.G, r0 = (tile - first_tile<kTileRows>(a, sp.s)) * kTileRows;
-  if (r0 >= rows) return;
-
-  // the keys that this lane's row sees
-  const int lim = sp.sees(a, min(r0 + 32 * wave + l32, rows - 1) / a.G);
-  const int wave_lo = __builtin_amdgcn_readfirstlane(lim);              // the wave's first row's
-  const int wave_hi = __builtin_amdgcn_readlane(lim, 31);               // and its last row's
-  const bool has_rows = r0 + 32 * wave < rows;
-  const int kb = sg.kt0 * BN;
-  const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kTileRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
-  const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
-  if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
-  __syncthreads();
-
-  u4 qf[KS];
-  {
-    const int row = min(r0 + 32 * wave + l32, rows - 1), tok = row / a.G;
-    const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = qp[2 * ks];
-  }
-  pf32x16 o[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
-  float m = -INFINITY, l = 0.f;   // in score units (before 1/sqrt(d)), over this lane's keys
-
-  GroupBases<PPR> bases;
-  u4 rk[NP], rv[NP];
-  auto load = [&](int j0, uint64_t pool, u4 (&to)[NP]) {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int x = i * kBlock + wave * kWave;    // the wave's first piece of this load
-      to[i] = load_at(bases.at(j0 / 16 + x / (16 * PPR)) + pool, (x % (16 * PPR) + lane) * 16);
+    Segment sg;
+    if constexpr (SHARES) {
+      sg = next_segment(a, s_sum, next, end);
+      if (sg.kt1 == 0) break;
+      if (seg) __syncthreads();      // the tile before is done with s_bad
+    } else {
+      sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};   // long ones first
+      next = end;
     }
-  };
-  auto stage = [&](int b, int j0) {
-    if (j0 + BN > least) {
-      const int tid = wave * kWave + lane_here();
+    const int tile = sg.tile, h = sg.h;
+    const bool whole = sg.whole;
+    const Span sp(a, cu, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, cu, s); }));
+    const int rows = sp.n * a.G, r0 = (tile - first_tile<kTileRows>(a, cu, sp.s)) * kTileRows;
+    if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
+
+    // the keys that this lane's row sees
+    const int lim = sp.sees(a, min(r0 + 32 * wave + l32, rows - 1) / a.G);
+    const int wave_lo = __builtin_amdgcn_readfirstlane(lim);              // the wave's first row's
+    const int wave_hi = __builtin_amdgcn_readlane(lim, 31);               // and its last row's
+    const bool has_rows = r0 + 32 * wave < rows;
+    const int kb = sg.kt0 * BN;
+    const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kTileRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
+    const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
+    if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+    __syncthreads();
+
+    u4 qf[KS];
+    {
+      const int row = min(r0 + 32 * wave + l32, rows - 1), tok = row / a.G;
+      const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = qp[2 * ks];
+    }
+    pf32x16 o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    float m = -INFINITY, l = 0.f;   // in score units (before 1/sqrt(d)), over this lane's keys
+
+    GroupBases<PPR> bases;
+    u4 rk[NP], rv[NP];
+    auto load = [&](int j0, uint64_t pool, u4 (&to)[NP]) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int x = i * kBlock + tid, key = j0 + x / PPR;
-        rv[i] = key < sp.L ? rv[i] : u4{0, 0, 0, 0};
-        scrub<T>(rv[i], key, x % PPR * (D / PPR), s_bad);
+        const int x = i * kBlock + wave * kWave;    // the wave's first piece of this load
+        to[i] = load_at(bases.at(j0 / 16 + x / (16 * PPR)) + pool, (x % (16 * PPR) + lane) * 16);
       }
-    }
+    };
+    auto stage = [&](int b, int j0) {
+      if (j0 + BN > least) {
+        const int tid = wave * kWave + lane_here();
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int x = i * kBlock + threadIdx.x;
-      s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
-      s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
-    }
-  };
+        for (int i = 0; i < NP; ++i) {
+          const int x = i * kBlock + tid, key = j0 + x / PPR;
+          rv[i] = key < sp.L ? rv[i] : u4{0, 0, 0, 0};
+          scrub<float>(rv[i], key, x % PPR * (D / PPR), s_bad);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int x = i * kBlock + threadIdx.x;
+        s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
+        s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
+      }
+    };
 
-  if (kb < ke) {
-    bases.fill(a, sp, h, kb / 16);
-    load(kb, 0, rk);
-    load(kb, to_v(a.c), rv);
-    stage(0, kb);
-  }
-  int buf = 0;
-  for (int j0 = kb; j0 < ke; j0 += BN, buf ^= 1) {
-    __syncthreads();
-    const bool more = j0 + BN < ke;
-    if (more) {
-      bases.reach(a, sp, h, (j0 + BN) / 16, (j0 + BN) / 16 + BN / 16 - 1);
-      load(j0 + BN, 0, rk);
-      load(j0 + BN, to_v(a.c), rv);
+    if (kb < ke) {
+      bases.fill(a, sp, h, kb / 16);
+      load(kb, 0, rk);
+      load(kb, to_v(a.c), rv);
+      stage(0, kb);
     }
-    if (has_rows && j0 < wave_hi) {
-      const u4* tk = s_k[buf];
-      const u4* tv = s_v[buf];
-      pf32x16 s[NS];
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if (ks % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // not every operand at once in registers
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          const u4 w = tk[S::k_at(32 * n + l32, 2 * ks + half)];
-          if constexpr (S::kBf16) {
-            s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, w),
-                                                           __builtin_bit_cast(pbf16x8, qf[ks]), s[n], 0, 0, 0);
-          } else {
-            s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w.x), __uint_as_float(qf[ks].x), s[n], 0, 0, 0);
-            s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w.y), __uint_as_float(qf[ks].y), s[n], 0, 0, 0);
-            s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w.z), __uint_as_float(qf[ks].z), s[n], 0, 0, 0);
-            s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w.w), __uint_as_float(qf[ks].w), s[n], 0, 0, 0);
-          }
-        }
+    int buf = 0;
+    for (int j0 = kb; j0 < ke; j0 += BN, buf ^= 1) {
+      __syncthreads();
+      const bool more = j0 + BN < ke;
+      if (more) {
+        bases.reach(a, sp, h, (j0 + BN) / 16, (j0 + BN) / 16 + BN / 16 - 1);
+        load(j0 + BN, 0, rk);
+        load(j0 + BN, to_v(a.c), rv);
       }
-      const bool masked = j0 + BN > wave_lo;
-      if (masked) {
-        const int left = here(lim) - j0 - 4 * half;
+      if (has_rows && j0 < wave_hi) {
+        const u4* tk = s_k[buf];
+        pf32x16 s;
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[n][i] = 32 * n + 8 * (i / 4) + i % 4 < left ? s[n][i] : -INFINITY;
-      }
-      float top = s[0][0];
+        for (int ks = 0; ks < KS; ++ks) {
+          if (ks % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // not every operand at once in registers
+          const u4 w = tk[S::k_at(l32, 2 * ks + half)];
 #pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-      top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      if (__ballot(top > m)) {
-        const float now = fmaxf(m, top);
-        const float alpha = m == -INFINITY ? 0.f : exp2_((m - now) * a.scale_log2);
-        m = now;
-        l *= alpha;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
-      }
-      const float mc = m == -INFINITY ? 0.f : m * a.scale_log2;
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][i] = exp2_(__builtin_fmaf(s[n][i], a.scale_log2, -mc));
-          l += s[n][i];
+          for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[i]), __uint_as_float(qf[ks][i]), s, 0, 0, 0);
         }
-      if constexpr (S::kBf16) {
-        // the lane's part of the transposed reads: key 4 half + (lane % 16) / 4 of 8, 8 bytes
-        // from output 16 (lane / 16 % 2) + 4 (lane % 4) on
-        const int kr = 4 * half + lane % 16 / 4, pc = 2 * (lane / 16 % 2) + lane % 4 / 2, by = lane % 2 * 8;
-        auto vt = [&](int kk, int b) {
-          return read_vt(tv, S::v_at(16 * kk + kr, 4 * b + pc) * 16 + by,
-                         S::v_at(16 * kk + 8 + kr, 4 * b + pc) * 16 + by);
-        };
-        // probabilities rounded to bf16 (to nearest, 2^-9 of each at most): their sum l is
-        // taken before, in fp32
-        pbf16x8 pb[2 * NS];
+        if (j0 + BN > wave_lo) {
+          const int left = here(lim) - j0 - 4 * half;
 #pragma unroll
-        for (int kk = 0; kk < 2 * NS; ++kk) {
-          pf32x8 x;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = s[kk / 2][8 * (kk % 2) + i];
-          pb[kk] = to_bf16x8(x);
+          for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < left ? s[i] : -INFINITY;
         }
+        float top = s[0];
 #pragma unroll
-        for (int kk = 0; kk < 2 * NS; ++kk)
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        if (__ballot(top > m)) {
+          const float now = fmaxf(m, top);
+          const float alpha = m == -INFINITY ? 0.f : exp2_((m - now) * a.scale_log2);
+          m = now;
+          l *= alpha;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt(kk, b), pb[kk], o[b], 0, 0, 0);
-      } else {
-        const float* tf = reinterpret_cast<const float*>(tv);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+        }
+        const float mc = m == -INFINITY ? 0.f : m * a.scale_log2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[i] = exp2_(__builtin_fmaf(s[i], a.scale_log2, -mc));
+          l += s[i];
+        }
+        const float* tv = reinterpret_cast<const float*>(s_v[buf]);
         auto vt = [&](int i, int b) {   // key of result element i, output 32 b + l32
           const int r = 8 * (i / 4) + 4 * half + i % 4;
-          return tf[S::v_at(r, 8 * b + l32 / 4) * 4 + l32 % 4];
+          return tv[S::v_at(r, 8 * b + l32 / 4) * 4 + l32 % 4];
         };
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(vt(i, b), s[0][i], o[b], 0, 0, 0);
+          for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(vt(i, b), s[i], o[b], 0, 0, 0);
         }
       }
+      if (more) stage(buf ^ 1, j0 + BN);
     }
-    if (more) stage(buf ^ 1, j0 + BN);
-  }
 
-  __syncthreads();   // s_bad
-  if (has_rows) {
-    l += __shfl_xor(l, 32, kWave);
-    const int lane = lane_here(), half = lane / 32, r = 32 * wave + lane % 32;
-    const int row = r0 + r, tok = row / a.G;
-    const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;
-    // a partial's place: a workgroup's first row tile, or its last
-    const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kTileRows + r;
-    const float mul = !whole ? 1.f : l > 0.f ? 1.f / l : l;   // no key: 0; NaN stays
-    if (half == 0 && row < rows) store_ml(a, whole ? nullptr : a.part_ml + slot * 2, at, m * a.scale_log2, l);
+    __syncthreads();   // s_bad
+    if (has_rows) {
+      l += __shfl_xor(l, 32, kWave);
+      const int lane = lane_here(), half = lane / 32, r = 32 * wave + lane % 32;
+      const int row = r0 + r, tok = row / a.G;
+      const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;
+      // a partial's place: a workgroup's first row tile, or its last
+      const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kTileRows + r;
+      const float mul = !whole ? 1.f : l > 0.f ? 1.f / l : l;   // no key: 0; NaN stays
+      if (half == 0 && row < rows) store_ml(a, whole ? nullptr : a.part_ml + slot * 2, at, m * a.scale_log2, l);
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 4 && row < rows; ++i) {
-        const int d0 = 32 * b + 8 * i + 4 * half;
-        float x[4];
+        for (int i = 0; i < 4 && row < rows; ++i) {
+          const int d0 = 32 * b + 8 * i + 4 * half;
+          float x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim ? __builtin_nanf("") : o[b][4 * i + e] * mul;
-        store4<T>(a, whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
-      }
-  }
+          for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim ? __builtin_nanf("") : o[b][4 * i + e] * mul;
+          store4<float>(a, whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
+        }
+    }
   }
 }
 
@@ -588,343 +562,391 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
   __shared__ u4 s_k[3][S::kPieces], s_v[3][S::kPieces];
   __shared__ int s_bad[D];
   __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
+  __shared__ int32_t s_cu[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int s_wave[kWaves];
 
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, half = lane / 32;
   const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int32_t* cu = SHARES ? s_cu : a.cu;
   int64_t next = 0, end = 1;
   if constexpr (SHARES) {
-    if (!share_out<BN, kWideRows>(a, id, s_sum, s_wave, next, end)) return;
+    if (!share_out<BN, kWideRows>(a, id, s_cu, s_sum, s_wave, next, end)) return;
   }
 
   for (int seg = 0; next < end; ++seg) {
-  Segment sg;
-  if constexpr (SHARES) {
-    sg = next_segment(a, s_sum, next, end);
-    if (seg) __syncthreads();      // the tile before is done with LDS
-  } else {
-    sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};
-    next = end;
-  }
-  const int h = sg.h;
-  const Span sp(a, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, s); }));
-  const int rows = sp.n * a.G, r0 = (sg.tile - first_tile<kWideRows>(a, sp.s)) * kWideRows;
-  if (r0 >= rows) return;
-
-  // the keys that this lane's two rows see
-  int lim[2];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) lim[c] = sp.sees(a, min(r0 + 64 * wave + 32 * c + l32, rows - 1) / a.G);
-  const int wave_lo = __builtin_amdgcn_readfirstlane(lim[0]);           // the wave's first row's
-  const int kb = sg.kt0 * BN;
-  const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kWideRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
-  const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
-  const int steps = max((ke - kb + BN - 1) / BN, 0) * 2;   // whole tiles: what lies behind is masked
-  if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
-  __syncthreads();
-
-  u4 qf[2][KS];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int row = min(r0 + 64 * wave + 32 * c + l32, rows - 1), tok = row / a.G;
-    const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qf[c][ks] = qp[2 * ks];
-      asm volatile("" : "+a"(qf[c][ks]));
+    Segment sg;
+    if constexpr (SHARES) {
+      sg = next_segment(a, s_sum, next, end);
+      if (sg.kt1 == 0) break;
+      if (seg) __syncthreads();      // the tile before is done with LDS
+    } else {
+      sg = Segment{a.n_tile - 1 - (int)(id % a.n_tile), (int)(id / a.n_tile), 0, 0x7fffffff, true};
+      next = end;
     }
-  }
-  pf32x16 o[NB][2];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[b][c][i] = 0.f;
-  // a row's reference m (in score units), mc (in log2 units), what a score must pass for m to
-  // follow, and the sum l over this lane's keys
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, alpha[2] = {1.f, 1.f};
-  float mc[2] = {0.f, 0.f}, pass[2] = {-INFINITY, -INFINITY};
-  bool grown = false;   // m has changed for the step in hand: O follows behind its V product
+    const int h = sg.h;
+    const Span sp(a, cu, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, cu, s); }));
+    const int rows = sp.n * a.G, r0 = (sg.tile - first_tile<kWideRows>(a, cu, sp.s)) * kWideRows;
+    if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
 
-  GroupBases<PPR> bases;
-  constexpr int kGroups = BN / 16;
-  u4 rk[NP], rv[NP];
-  uint64_t at_k[NP], at_v[NP];   // a tile's addresses: K's loads find them, V's follow a tile later
-  const uint64_t kv = to_v(a.c);
-  const uint32_t offset = (wave * kWave % (16 * PPR) + lane) * 16;
-  auto reach = [&](int j0) INLINE { bases.reach(a, sp, h, j0 / 16, j0 / 16 + kGroups - 1); };
-  auto load_k = [&](int j0, int i) INLINE {   // behind reach()
-    at_v[i] = at_k[i] + kv;
-    at_k[i] = bases.at(j0 / 16 + (i * kBlock + wave * kWave) / (16 * PPR));
-    rk[i] = load_at(at_k[i], offset);
-  };
-  auto load_v = [&](int i) INLINE { rv[i] = load_at(at_v[i], offset); };
-  auto put_k = [&](int b, int i) INLINE {
-    const int x = i * kBlock + threadIdx.x;
-    s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
-  };
-  auto put_v = [&](int b, int i) INLINE {
-    const int x = i * kBlock + threadIdx.x;
-    s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
-  };
-  auto clean_v = [&](int j0) INLINE {
-    if (j0 + BN > least) {
-      const int tid = wave * kWave + lane_here();
+    // the keys that this lane's two rows see
+    int lim[2];
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int x = i * kBlock + tid, key = j0 + x / PPR;
-        rv[i] = key < sp.L ? rv[i] : u4{0, 0, 0, 0};
-        scrub<bf16_t>(rv[i], key, x % PPR * (D / PPR), s_bad);
-      }
+    for (int c = 0; c < 2; ++c) lim[c] = sp.sees(a, min(r0 + 64 * wave + 32 * c + l32, rows - 1) / a.G);
+    const int wave_lo = __builtin_amdgcn_readfirstlane(lim[0]);           // the wave's first row's
+    const int kb = sg.kt0 * BN;
+    const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kWideRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
+    const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
+    const int steps = max((ke - kb + BN - 1) / BN, 0) * 2;   // whole tiles: what lies behind is masked
+    if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+    __syncthreads();
+
+    u4 qf[2][KS];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int row = min(r0 + 64 * wave + 32 * c + l32, rows - 1), tok = row / a.G;
+      const u4* qp = a.q + (int64_t)(sp.c0 + tok) * a.q_u4 + (int64_t)(h * a.G + row - tok * a.G) * PPR + half;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[c][ks] = qp[2 * ks];
     }
-  };
-  // V^T operand of keys 32 x + 16 kk on, outputs 32 b on
-  const int kr = 4 * half + lane % 16 / 4, pc = 2 * (lane / 16 % 2) + lane % 4 / 2, by = lane % 2 * 8;
-  auto vt = [&](const u4* tv, int x, int kk, int b) INLINE {
-    return read_vt(tv, S::v_at(32 * x + 16 * kk + kr, 4 * b + pc) * 16 + by,
-                   S::v_at(32 * x + 16 * kk + 8 + kr, 4 * b + pc) * 16 + by);
-  };
-  // O stays in AGPRs, which leaves the other registers to what the VALU works on.  The compiler
-  // does not see these as MFMAs: o_ready() keeps O's readers behind them.
-  auto add_product = [&](const pbf16x8& v, const pbf16x8& p, pf32x16& x) INLINE {
-    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(p));
-  };
-  auto o_ready = [&]() INLINE {   // 32 wait states (19 needed behind the last MFMA)
+    pf32x16 o[NB][2];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(o[b][0]), "+a"(o[b][1]));
-  };
-  float top[2] = {0.f, 0.f};
-  u4 kf[KS];   // K operands of the next step
-  auto k_operand = [&](const u4* tk, int x, int ks) INLINE { kf[ks] = tk[S::k_at(32 * x + l32, 2 * ks + half)]; };
-  // One step: scores of the next 32 keys (kf) into `next`, the probabilities of the scores in
-  // `cur` (pn), the V product of those before (pp), and the K operands of the step after it
-  // (rows 32 kx on of tk).  Written out MFMA by MFMA, with what fits beside each: an MFMA takes
-  // the pipe for 32 cycles, in which the wave can issue 7 other instructions.  A lane's element
-  // goes through three of these places (argument, exponential, rounding), so that none of its
-  // parts waits for the one before.  Probabilities are rounded to bf16 (to nearest, 2^-8 of each
-  // at most); their sum is taken before, in fp32.
-  auto step = [&](const u4* tk, int kx, const u4* tv, int vx, pf32x16 (&cur)[2], pf32x16 (&next)[2],
-                  const u4 (&pp)[2][2], u4 (&pn)[2][2], auto beside) INLINE {
-    constexpr int Q = 2 * KS, V = 4 * NB, E = 32;      // MFMAs of each kind, elements of a lane
-    constexpr int per = E / (Q + V);                   // elements beside an MFMA
-    pbf16x8 vf[2][NB];
-    auto part0 = [&](auto e) INLINE {
-      if constexpr (e < E) cur[e / 16][e % 16] = __builtin_fmaf(cur[e / 16][e % 16], a.scale_log2, -mc[e / 16]);
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][c][i] = 0.f;
+    // a row's reference m (in score units), mc (in log2 units), what a score must pass for m to
+    // follow, and the sum l over this lane's keys
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, alpha[2] = {1.f, 1.f};
+    float mc[2] = {0.f, 0.f}, pass[2] = {-INFINITY, -INFINITY};
+    bool grown = false;   // m has changed for the step in hand: O follows behind its V product
+
+    GroupBases<PPR> bases;
+    constexpr int kGroups = BN / 16;
+    u4 rk[NP], rv[NP];
+    uint64_t at_k[NP], at_v[NP];   // a tile's addresses: K's loads find them, V's follow a tile later
+    const uint64_t kv = to_v(a.c);
+    const uint32_t offset = (wave * kWave % (16 * PPR) + lane) * 16;
+    auto reach = [&](int j0) INLINE { bases.reach(a, sp, h, j0 / 16, j0 / 16 + kGroups - 1); };
+    auto load_k = [&](int j0, int i) INLINE {   // behind reach()
+      at_v[i] = at_k[i] + kv;
+      at_k[i] = bases.at(j0 / 16 + (i * kBlock + wave * kWave) / (16 * PPR));
+      rk[i] = load_at(at_k[i], offset);
     };
-    auto part1 = [&](auto e) INLINE {
-      if constexpr (e < E) cur[e / 16][e % 16] = exp2_(cur[e / 16][e % 16]);
+    auto load_v = [&](int i) INLINE { rv[i] = load_at(at_v[i], offset); };
+    auto put_k = [&](int b, int i) INLINE {
+      const int x = i * kBlock + threadIdx.x;
+      s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
     };
-    auto part2 = [&](auto e) INLINE {
-      constexpr int c = e / 16, i = e % 16;
-      l[c] += cur[c][i];
-      asm volatile("" : "+v"(l[c]));   // here, not behind the step
-      if constexpr (i % 2 == 1) {
-        typedef float f2 __attribute__((ext_vector_type(2)));
-        const pbf16x2 y = __builtin_convertvector(f2{cur[c][i - 1], cur[c][i]}, pbf16x2);
-        pn[i / 8][c][i % 8 / 2] = __builtin_bit_cast(uint32_t, y);
+    auto put_v = [&](int b, int i) INLINE {
+      const int x = i * kBlock + threadIdx.x;
+      s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
+    };
+    auto clean_v = [&](int j0) INLINE {
+      if (j0 + BN > least) {
+        const int tid = wave * kWave + lane_here();
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int x = i * kBlock + tid, key = j0 + x / PPR;
+          rv[i] = key < sp.L ? rv[i] : u4{0, 0, 0, 0};
+          scrub<bf16_t>(rv[i], key, x % PPR * (D / PPR), s_bad);
+        }
       }
     };
-    auto elements = [&](auto n) INLINE {
-      each<per>([&](auto y) INLINE {
-        part2(std::integral_constant<int, per * n + y>());
-        part1(std::integral_constant<int, per * n + y + per>());
-        part0(std::integral_constant<int, per * n + y + 2 * per>());
-      });
+    // V^T operand of keys 32 x + 16 kk on, outputs 32 b on
+    const int kr = 4 * half + lane % 16 / 4, pc = 2 * (lane / 16 % 2) + lane % 4 / 2, by = lane % 2 * 8;
+    auto vt = [&](const u4* tv, int x, int kk, int b) INLINE {
+      return read_vt(tv, S::v_at(32 * x + 16 * kk + kr, 4 * b + pc) * 16 + by,
+                     S::v_at(32 * x + 16 * kk + 8 + kr, 4 * b + pc) * 16 + by);
     };
+    // O stays in AGPRs, which leaves the other registers to what the VALU works on.  The compiler
+    // does not see these as MFMAs: o_ready() keeps O's readers behind them.
+    auto add_product = [&](const pbf16x8& v, const pbf16x8& p, pf32x16& x) INLINE {
+      asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(p));
+    };
+    auto o_ready = [&]() INLINE {   // 32 wait states (19 needed behind the last MFMA)
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) next[c][i] = 0.f;
-    each<2 * per>([&](auto e) INLINE { part0(e); });
-    each<per>([&](auto e) INLINE { part1(e); });
-    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the K operands, all in one wait
-    __builtin_amdgcn_sched_barrier(0);
-    each<Q>([&](auto n) INLINE {
-      constexpr int ks = n / 2, c = n % 2, x = n - Q / 2;
-      next[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
-                                                        __builtin_bit_cast(pbf16x8, qf[c][ks]), next[c], 0, 0, 0);
-      if constexpr (x >= 0 && x < 2 * NB) vf[x / NB][x % NB] = vt(tv, vx, x / NB, x % NB);
-      if constexpr (x < 0) beside(n);
-      elements(n);
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    each<V>([&](auto n) INLINE {
-      constexpr int kk = n / (2 * NB), b = n / 2 % NB, c = n % 2;
-      add_product(vf[kk][b], __builtin_bit_cast(pbf16x8, pp[kk][c]), o[b][c]);
-      if constexpr (n % 2 == 0 && n / 2 < KS) k_operand(tk, kx, n / 2);
-      elements(std::integral_constant<int, Q + decltype(n)::value>());
-      // the highest of the next scores, from behind their last MFMA on
-      if constexpr (n >= 2) {
-        constexpr int most = ((E + V - 3) / (V - 2) + 1) / 2 * 2;
-        constexpr int e0 = (n - 2) * most, e1 = (n - 1) * most < E ? (n - 1) * most : E;
-        each<(e1 > e0 ? e1 - e0 : 0)>([&](auto y) INLINE {
-          constexpr int e = e0 + y;
-          top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], next[e / 16][e % 16]) : next[e / 16][0];
+      for (int b = 0; b < NB; ++b) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(o[b][0]), "+a"(o[b][1]));
+    };
+    float top[2] = {0.f, 0.f};
+    u4 kf[KS];   // K operands of the next step
+    auto k_operand = [&](const u4* tk, int x, int ks) INLINE { kf[ks] = tk[S::k_at(32 * x + l32, 2 * ks + half)]; };
+    // One step: scores of the next 32 keys (kf) into `next`, the probabilities of the scores in
+    // `cur` (pn), the V product of those before (pp), and the K operands of the step after it
+    // (rows 32 kx on of tk).  Written out MFMA by MFMA, with what fits beside each: an MFMA takes
+    // the pipe for 32 cycles, in which the wave can issue 7 other instructions.  A lane's element
+    // goes through three of these places (argument, exponential, rounding), so that none of its
+    // parts waits for the one before.  Probabilities are rounded to bf16 (to nearest, 2^-8 of each
+    // at most); their sum is taken before, in fp32.
+    auto step = [&](const u4* tk, int kx, const u4* tv, int vx, pf32x16 (&cur)[2], pf32x16 (&next)[2],
+                    const u4 (&pp)[2][2], u4 (&pn)[2][2], auto beside) INLINE {
+      constexpr int Q = 2 * KS, V = 4 * NB, E = 32;      // MFMAs of each kind, elements of a lane
+      constexpr int per = E / (Q + V);                   // elements beside an MFMA
+      pbf16x8 vf[2][NB];
+      auto part0 = [&](auto e) INLINE {
+        if constexpr (e < E) cur[e / 16][e % 16] = __builtin_fmaf(cur[e / 16][e % 16], a.scale_log2, -mc[e / 16]);
+      };
+      auto part1 = [&](auto e) INLINE {
+        if constexpr (e < E) cur[e / 16][e % 16] = exp2_(cur[e / 16][e % 16]);
+      };
+      auto part2 = [&](auto e) INLINE {
+        constexpr int c = e / 16, i = e % 16;
+        l[c] += cur[c][i];
+        asm volatile("" : "+v"(l[c]));   // here, not behind the step
+        if constexpr (i % 2 == 1) {
+          typedef float f2 __attribute__((ext_vector_type(2)));
+          const pbf16x2 y = __builtin_convertvector(f2{cur[c][i - 1], cur[c][i]}, pbf16x2);
+          pn[i / 8][c][i % 8 / 2] = __builtin_bit_cast(uint32_t, y);
+        }
+      };
+      auto elements = [&](auto n) INLINE {
+        each<per>([&](auto y) INLINE {
+          part2(std::integral_constant<int, per * n + y>());
+          part1(std::integral_constant<int, per * n + y + per>());
+          part0(std::integral_constant<int, per * n + y + 2 * per>());
         });
-        asm volatile("" : "+v"(top[0]), "+v"(top[1]));   // here, not behind the step
-      }
+      };
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[c][i] = 0.f;
+      each<2 * per>([&](auto e) INLINE { part0(e); });
+      each<per>([&](auto e) INLINE { part1(e); });
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the K operands, all in one wait
       __builtin_amdgcn_sched_barrier(0);
-    });
+      each<Q>([&](auto n) INLINE {
+        constexpr int ks = n / 2, c = n % 2, x = n - Q / 2;
+        next[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
+                                                          __builtin_bit_cast(pbf16x8, qf[c][ks]), next[c], 0, 0, 0);
+        if constexpr (x >= 0 && x < 2 * NB) vf[x / NB][x % NB] = vt(tv, vx, x / NB, x % NB);
+        if constexpr (x < 0) beside(n);
+        elements(n);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      each<V>([&](auto n) INLINE {
+        constexpr int kk = n / (2 * NB), b = n / 2 % NB, c = n % 2;
+        add_product(vf[kk][b], __builtin_bit_cast(pbf16x8, pp[kk][c]), o[b][c]);
+        if constexpr (n % 2 == 0 && n / 2 < KS) k_operand(tk, kx, n / 2);
+        elements(std::integral_constant<int, Q + decltype(n)::value>());
+        // the highest of the next scores, from behind their last MFMA on
+        if constexpr (n >= 2) {
+          constexpr int most = ((E + V - 3) / (V - 2) + 1) / 2 * 2;
+          constexpr int e0 = (n - 2) * most, e1 = (n - 1) * most < E ? (n - 1) * most : E;
+          each<(e1 > e0 ? e1 - e0 : 0)>([&](auto y) INLINE {
+            constexpr int e = e0 + y;
+            top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], next[e / 16][e % 16]) : next[e / 16][0];
+          });
+          asm volatile("" : "+v"(top[0]), "+v"(top[1]));   // here, not behind the step
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) asm volatile("" : "+v"(pn[kk][c]));
-  };
-  // a step's scores masked, and its reference: keys from j on
-  auto settle = [&](pf32x16 (&s)[2], int j, bool first = false) INLINE {
-    if (first || j + 32 > min(wave_lo, ke)) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int left = min(here(lim[c]), ke) - j - 4 * half;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[c][i] = 8 * (i / 4) + i % 4 < left ? s[c][i] : -INFINITY;
-        top[c] = s[c][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top[c] = __builtin_elementwise_maximum(top[c], s[c][i]);
-      }
-    }
-    grown = __ballot(top[0] > pass[0] || top[1] > pass[1]) != 0;
-    if (grown) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const float now = fmaxf(m[c], fmaxf(top[c], __shfl_xor(top[c], 32, kWave)));
-        alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
-        m[c] = now;
-        mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
-        pass[c] = now + 8.f / a.scale_log2;
-        l[c] *= alpha[c];
-      }
-    }
-  };
-  auto follow = [&]() INLINE {
-    if (grown) {
-      o_ready();
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
+        for (int kk = 0; kk < 2; ++kk) asm volatile("" : "+v"(pn[kk][c]));
+    };
+    // a step's scores masked, and its reference: keys from j on
+    auto settle = [&](pf32x16 (&s)[2], int j, bool first = false) INLINE {
+      if (first || j + 32 > min(wave_lo, ke)) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
+          const int left = min(here(lim[c]), ke) - j - 4 * half;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[b][c][i] *= alpha[c];
-          asm volatile("s_nop 7" : "+a"(o[b][c]));
+          for (int i = 0; i < 16; ++i) s[c][i] = 8 * (i / 4) + i % 4 < left ? s[c][i] : -INFINITY;
+          top[c] = s[c][0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top[c] = __builtin_elementwise_maximum(top[c], s[c][i]);
         }
-    }
-  };
-
-  if (steps > 0) {
-    bases.fill(a, sp, h, kb / 16);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) at_k[i] = 0;
-    auto load_tile = [&](int j0) INLINE {
-      reach(j0);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) load_k(j0, i);
-    };
-    load_tile(kb);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) rv[i] = load_at(at_k[i] + kv, offset);
-    clean_v(kb);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      put_k(0, i);
-      put_v(0, i);
-      put_v(2, i);                // for step 0's product, with probabilities of 0
-    }
-    load_tile(kb + BN);           // behind the last key: the last group again
-#pragma unroll
-    for (int i = 0; i < NP; ++i) put_k(1, i);
-    load_tile(kb + 2 * BN);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) load_v(i);
-    __syncthreads();
-    pf32x16 s0[2], s1[2];
-    u4 p0[2][2], p1[2][2];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) p1[kk][c] = u4{0, 0, 0, 0};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 0, ks);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s0[c][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        s0[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
-                                                        __builtin_bit_cast(pbf16x8, qf[c][ks]), s0[c], 0, 0, 0);
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 1, ks);
-    settle(s0, kb, true);
-    // 64 keys.  Of K, tile b and the next are read and the one behind it written; of V, the
-    // tile before, tile b, and the next: three buffers of each, one barrier.
-    auto stage = [&](auto buffer, int j0) INLINE {
-      constexpr int b = decltype(buffer)::value, b1 = (b + 1) % 3, b2 = (b + 2) % 3;
-      __syncthreads();
-      // a tile's loads right behind the stores of the one before: nearly two steps ahead
-      reach(j0 + 3 * BN);
-      step(s_k[b1], 0, s_v[b2], 1, s0, s1, p1, p0, [&](auto n) INLINE {
-        if constexpr (n < NP) put_k(b2, n);
-        else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
-      });
-      follow();
-      settle(s1, j0 + 32);
-      clean_v(j0 + BN);
-      step(s_k[b1], 1, s_v[b], 0, s1, s0, p0, p1, [&](auto n) INLINE {
-        if constexpr (n < NP) put_v(b1, n);
-        else if constexpr (n < 2 * NP) load_v(n - NP);
-      });
-      follow();
-      settle(s0, j0 + 64);
-    };
-    for (int t = 0; t < steps; t += 6) {
-      stage(std::integral_constant<int, 0>(), kb + 32 * t);
-      if (t + 2 >= steps) break;
-      stage(std::integral_constant<int, 1>(), kb + 32 * t + 64);
-      if (t + 4 >= steps) break;
-      stage(std::integral_constant<int, 2>(), kb + 32 * t + 128);
-    }
-    const u4* tv = s_v[(steps / 2 - 1) % 3];   // the last step's product
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const pbf16x8 w = vt(tv, 1, kk, b);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) add_product(w, __builtin_bit_cast(pbf16x8, p1[kk][c]), o[b][c]);
       }
-    o_ready();
-  }
-
-  __syncthreads();   // s_bad
-  {
+      grown = __ballot(top[0] > pass[0] || top[1] > pass[1]) != 0;
+      if (grown) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      l[c] += __shfl_xor(l[c], 32, kWave);
-      const int lane = lane_here(), half = lane / 32, r = 64 * wave + 32 * c + lane % 32;
-      const int row = r0 + r, tok = row / a.G;
-      const int64_t at = (int64_t)(sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;
-      // a partial's place: a workgroup's first row tile, or its last
-      const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kWideRows + r;
-      const float mul = !sg.whole ? 1.f : l[c] > 0.f ? 1.f / l[c] : l[c];   // no key: 0; NaN stays
-      if (row < rows) {
-        if (half == 0) store_ml(a, sg.whole ? nullptr : a.part_ml + slot * 2, at, m[c] * a.scale_log2, l[c]);
+        for (int c = 0; c < 2; ++c) {
+          // a row whose own maximum has not passed stays as it is: no row's result hangs on another's
+          const float both = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
+          const float now = both > pass[c] ? both : m[c];
+          alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
+          m[c] = now;
+          mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
+          pass[c] = now + 8.f / a.scale_log2;
+          l[c] *= alpha[c];
+        }
+      }
+    };
+    auto follow = [&]() INLINE {
+      if (grown) {
+        o_ready();
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int d0 = 32 * b + 8 * i + 4 * half;
-            float x[4];
+          for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim[c] ? __builtin_nanf("") : o[b][c][4 * i + e] * mul;
-            store4<bf16_t>(a, sg.whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
+            for (int i = 0; i < 16; ++i) o[b][c][i] *= alpha[c];
+            asm volatile("s_nop 7" : "+a"(o[b][c]));
           }
       }
+    };
+
+    if (steps > 0) {
+      bases.fill(a, sp, h, kb / 16);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) at_k[i] = 0;
+      auto load_tile = [&](int j0) INLINE {
+        reach(j0);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) load_k(j0, i);
+      };
+      u4 rk1[NP];
+      load_tile(kb + BN);           // behind the last key: the last group again
+#pragma unroll
+      for (int i = 0; i < NP; ++i) rk1[i] = rk[i];
+      load_tile(kb);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) rv[i] = load_at(at_k[i] + kv, offset);
+      // Q stays in AGPRs
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[c][ks]));
+      clean_v(kb);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        put_k(0, i);
+        put_v(0, i);
+        put_v(2, i);                // for step 0's product, with probabilities of 0
+        rk[i] = rk1[i];
+        put_k(1, i);
+        at_k[i] = bases.at((kb + BN) / 16 + (i * kBlock + wave * kWave) / (16 * PPR));
+      }
+      load_tile(kb + 2 * BN);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) load_v(i);
+      __syncthreads();
+      pf32x16 s0[2], s1[2];
+      u4 p0[2][2], p1[2][2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) p1[kk][c] = u4{0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 0, ks);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s0[c][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          s0[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
+                                                          __builtin_bit_cast(pbf16x8, qf[c][ks]), s0[c], 0, 0, 0);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) k_operand(s_k[0], 1, ks);
+      settle(s0, kb, true);
+      // 64 keys.  Of K, tile b and the next are read and the one behind it written; of V, the
+      // tile before, tile b, and the next: three buffers of each, one barrier.
+      auto stage = [&](auto buffer, int j0) INLINE {
+        constexpr int b = decltype(buffer)::value, b1 = (b + 1) % 3, b2 = (b + 2) % 3;
+        __syncthreads();
+        // a tile's loads right behind the stores of the one before: nearly two steps ahead
+        reach(j0 + 3 * BN);
+        step(s_k[b1], 0, s_v[b2], 1, s0, s1, p1, p0, [&](auto n) INLINE {
+          if constexpr (n < NP) put_k(b2, n);
+          else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
+        });
+        follow();
+        settle(s1, j0 + 32);
+        clean_v(j0 + BN);
+        step(s_k[b1], 1, s_v[b], 0, s1, s0, p0, p1, [&](auto n) INLINE {
+          if constexpr (n < NP) put_v(b1, n);
+          else if constexpr (n < 2 * NP) load_v(n - NP);
+        });
+        follow();
+        settle(s0, j0 + 64);
+      };
+      for (int t = 0; t < steps; t += 6) {
+        stage(std::integral_constant<int, 0>(), kb + 32 * t);
+        if (t + 2 >= steps) break;
+        stage(std::integral_constant<int, 1>(), kb + 32 * t + 64);
+        if (t + 4 >= steps) break;
+        stage(std::integral_constant<int, 2>(), kb + 32 * t + 128);
+      }
+      const u4* tv = s_v[(steps / 2 - 1) % 3];   // the last step's product
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const pbf16x8 w = vt(tv, 1, kk, b);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) add_product(w, __builtin_bit_cast(pbf16x8, p1[kk][c]), o[b][c]);
+        }
+      o_ready();
     }
-  }
+
+    __syncthreads();   // s_bad; and K and V are read
+    // Out by way of LDS, 32 rows at a time: a lane's 4 outputs of each block make stores of whole
+    // lines there, and straight from registers took 8 us, 4 times as long.
+    {
+      const int lane = lane_here(), l32 = lane % 32, half = lane / 32;
+      u4* room = (wave < 2 ? s_k[0] : s_v[0]) + wave % 2 * (32 * D / 4);   // of this wave
+      if (__ballot(s_bad[lane % D] < ke || s_bad[D - kWave + lane] < ke)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (s_bad[32 * b + 8 * (i / 4) + 4 * half + i % 4] < lim[c]) o[b][c][i] = __builtin_nanf("");
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        l[c] += __shfl_xor(l[c], 32, kWave);
+        const int r = 64 * wave + 32 * c, left = rows - r0 - r;   // rows from r on
+        const int row = r0 + r + l32, tok = row / a.G;
+        const int at = (sp.c0 + tok) * a.HG + h * a.G + row - tok * a.G;   // T H G fits
+        // a partial's place: a workgroup's first row tile, or its last
+        const int64_t slot = ((int64_t)id * 2 + (seg > 0)) * kWideRows + r;
+        const float mul = !sg.whole ? 1.f : l[c] > 0.f ? 1.f / l[c] : l[c];   // no key: 0; NaN stays
+        if (half == 0 && l32 < left)
+          store_ml(a, sg.whole ? nullptr : a.part_ml + (slot + l32) * 2, at, m[c] * a.scale_log2, l[c]);
+        auto put = [&](auto f) INLINE {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              pf32x4 x;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = o[b][c][4 * i + e] * mul;
+              f(4 * b + i, x);
+            }
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        };
+        // rows of P pieces, permuted so that 16 rows' writes and a row's reads take all banks
+        auto place = [&](int r, int p, int P) INLINE { return r * P + (p ^ (r & (P < 16 ? P - 1 : 15))); };
+        if (sg.whole) {
+          put([&](int q, pf32x4 x) INLINE {
+            const pbf16x4 y = __builtin_convertvector(x, pbf16x4);
+            reinterpret_cast<uint64_t*>(room + place(l32, q, PPR))[half] = __builtin_bit_cast(uint64_t, y);
+          });
+#pragma unroll
+          for (int i = 0; i < 32 * PPR / kWave; ++i) {
+            const int r = (i * kWave + lane) / PPR, q = lane % PPR;
+            const int64_t to = __shfl(at, r, kWave);
+            if (r < left) static_cast<u4*>(a.out)[to * PPR + q] = room[place(r, q, PPR)];
+          }
+        } else {
+          constexpr int P = D / 4;
+          put([&](int q, pf32x4 x) INLINE { room[place(l32, 2 * q + half, P)] = __builtin_bit_cast(u4, x); });
+#pragma unroll
+          for (int i = 0; i < 32 * P / kWave; ++i) {
+            const int r = (i * kWave + lane) / P, q = lane % P;
+            if (r < left) reinterpret_cast<u4*>(a.part_o)[(slot + r) * P + q] = room[place(r, q, P)];
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");   // read before the next rows
+      }
+    }
   }
 }
 
@@ -940,7 +962,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
   if (sum1 <= sum0) return;
   const Shares sh(a, per_head);
   const int64_t x0 = (int64_t)h * per_head + sum0, x1 = (int64_t)h * per_head + sum1;
-  const int first = sh.of(x0), last = sh.of(x1 - 1);
+  const int first = sh.of(x0 + kSetup), last = sh.of(x1 - 1);
   if (first == last) return;   // whole: already written
   // the first part's partial is that of its last row tile if it began before this one; the others
   // begin in it
@@ -948,7 +970,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
   const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<R>(a, s); }));
   const int r0 = (tile - first_tile<R>(a, sp.s)) * R;
   const int d0 = threadIdx.x % TPR * 4, r = (int)(blockIdx.x % kPer) * RPB + threadIdx.x / TPR;
-  if (r0 + r >= sp.n * a.G) return;
+  if (r0 < 0 || r0 + r >= sp.n * a.G) return;
   auto place = [&](int i) { return (i == first ? place0 : (int64_t)i * 2 * R) + r; };
   auto ml = [&](int i) { return *reinterpret_cast<const float2*>(a.part_ml + place(i) * 2); };
   float top = -INFINITY;
@@ -1029,13 +1051,12 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   const int tile = (int)(id / a.n_split) / a.c.H;
   const Span sp(a, a.by_slot ? tile : find_slot(a.c.S, tile, [&](int s) { return first_tile<kFewRows>(a, s); }));
   const int r0 = a.by_slot ? 0 : (tile - first_tile<kFewRows>(a, sp.s)) * kFewRows;
-  const int rows = min(sp.n * a.G - r0, kFewRows);   // of this tile
-  if (rows <= 0) return;
-  // more tokens than max_new said
-  if (a.by_slot && sp.n * a.G > kFewRows) {
+  if (a.by_slot && sp.n * a.G > kFewRows) {   // more tokens than max_new said
     if (threadIdx.x == 0 && a.status) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
     return;
   }
+  const int rows = min(sp.n * a.G - r0, kFewRows);   // of this tile
+  if (r0 < 0 || rows <= 0) return;   // none; r0 < 0: cu that falls
   const int row = r0 + min(l16, rows - 1);
   const int tok = row / a.G, g = row - tok * a.G;
   const int lim = sp.sees(a, tok);
@@ -1149,7 +1170,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
       pf32x8 x;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4];
-      const pbf16x8 pb = to_bf16x8(x);   // rounded as in the tile kernel
+      const pbf16x8 pb = __builtin_convertvector(x, pbf16x8);   // rounded as in the wide kernel
 #pragma unroll
       for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt(b), pb, o[b], 0, 0, 0);
     } else {
@@ -1249,27 +1270,29 @@ __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
 }
 
 template <typename T, int D>
-hipError_t launch_td(AttnArgs a, const PageAttnPlan& pl, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.T * a.HG;
-  const dim3 each((unsigned)((rows + kWaves - 1) / kWaves)), block(kBlock);   // a wave to a row
+hipError_t launch_td(const AttnArgs& a, const PageAttnPlan& pl, hipStream_t stream) {
+  constexpr bool kWide = std::is_same<T, bf16_t>::value;
+  constexpr int R = kWide ? kWideRows : kTileRows;
+  const dim3 block(kBlock);
   if (pl.few) {
     hipLaunchKernelGGL((page_few_kernel<T, D>), dim3((unsigned)(a.n_tile * a.c.H * a.n_split)), block, 0, stream, a);
-    if (a.n_split > 1) hipLaunchKernelGGL((page_combine_kernel<T, D>), each, block, 0, stream, a);
-  } else {
-    constexpr bool kWide = std::is_same<T, bf16_t>::value;
-    constexpr int R = kWide ? kWideRows : kTileRows;
-    const dim3 grid(pl.shares ? pl.shares : (unsigned)(a.n_tile * a.c.H));
-    if constexpr (kWide) {
-      if (pl.shares) hipLaunchKernelGGL((page_wide_kernel<D, true>), grid, block, 0, stream, a);
-      else hipLaunchKernelGGL((page_wide_kernel<D, false>), grid, block, 0, stream, a);
-    } else {
-      if (pl.shares) hipLaunchKernelGGL((page_tile_kernel<T, D, true>), grid, block, 0, stream, a);
-      else hipLaunchKernelGGL((page_tile_kernel<T, D, false>), grid, block, 0, stream, a);
-    }
-    if (pl.shares)
-      hipLaunchKernelGGL((page_join_kernel<T, D, R>), dim3((unsigned)(a.n_tile * a.c.H * (R * D / 4 / kBlock))), block,
-                         0, stream, a);
+    // a wave per row
+    if (a.n_split > 1)
+      hipLaunchKernelGGL((page_combine_kernel<T, D>), dim3((unsigned)(((int64_t)a.T * a.HG + kWaves - 1) / kWaves)),
+                         block, 0, stream, a);
+    return hipGetLastError();
   }
+  const dim3 grid(a.shares ? a.shares : (unsigned)(a.n_tile * a.c.H));
+  if constexpr (kWide) {
+    if (a.shares) hipLaunchKernelGGL((page_wide_kernel<D, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((page_wide_kernel<D, false>), grid, block, 0, stream, a);
+  } else {
+    if (a.shares) hipLaunchKernelGGL((page_tile_kernel<D, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((page_tile_kernel<D, false>), grid, block, 0, stream, a);
+  }
+  if (a.shares)
+    hipLaunchKernelGGL((page_join_kernel<T, D, R>), dim3((unsigned)(a.n_tile * a.c.H * (R * D / 4 / kBlock))), block, 0,
+                       stream, a);
   return hipGetLastError();
 }
 
@@ -1277,13 +1300,16 @@ hipError_t launch_td(AttnArgs a, const PageAttnPlan& pl, hipStream_t stream) {
 
 PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int max_len) {
   PageAttnPlan p{};
-  const int slots = c.S < T ? c.S : T;      // that can have tokens
-  const size_t rows = (size_t)T * c.H * G;
-  p.by_slot = (int64_t)max_new * G <= kFewRows;
-  p.few = p.by_slot;
+  const bool wide = c.dtype == VASE_BF16;
+  const int slots = std::min(c.S, T);          // that can have tokens
+  const int64_t most = (int64_t)max_new * G;   // rows of a slot
+  const double reads = (double)((int64_t)T * G / kFewRows + slots) * c.H * max_len * c.d;   // of K by 16-row tiles
+  p.by_slot = most <= kFewRows;
+  p.few = most <= (wide ? 32 : 64) || reads <= 1 << 25;
   p.n_split = 1;
   p.keys = max_len;
   if (p.few) {
+    const size_t rows = (size_t)T * c.H * G;
     p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + c.S;
     // at least 256 keys to a range, up to kMaxSplit ranges
     const int64_t wgs = (p.by_slot ? slots : (int64_t)T * G / kFewRows + 1) * c.H;
@@ -1299,15 +1325,14 @@ PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int 
     }
     return p;
   }
-  const bool wide = c.dtype == VASE_BF16;
   const int R = wide ? kWideRows : kTileRows;
   p.n_tile = (int)((int64_t)T * G / R) + c.S;
-  // Shared out below 640 row tiles.
-  // The sums of 32-key tiles stay in 32 bits.
-  const int64_t tiles = ((int64_t)T * G / R + 1) * c.H;
-  if (tiles < 640 && p.n_tile <= kMaxTiles && max_len > 1024 &&
-      (int64_t)p.n_tile * (c.M * c.page / 32 + 1) <= 0x7fffffff) {
-    p.shares = 256 * (wide ? 1 : tile_waves(false, c.d));
+  const int shares = 256 * (wide ? 1 : tile_waves(c.d));   // workgroups that run at once
+  const int64_t tiles = ((int64_t)T * G / R + 1) * c.H, most_tiles = max_new <= max_len / 2 ? shares * 3 / 2 : shares;
+  // the sums of 32-key tiles stay in 32 bits
+  if (tiles <= most_tiles && p.n_tile <= kMaxTiles && max_len > 1024 &&
+      (int64_t)p.n_tile * (c.M * c.page / 32 + 1 + kSetup) <= 0x7fffffff) {
+    p.shares = shares;
     const size_t part = (size_t)p.shares * 2 * R;
     p.off_ml = part * c.d * sizeof(float);
     p.off_sums = p.off_ml + part * 2 * sizeof(float);
@@ -1331,8 +1356,8 @@ hipError_t launch_page_attn(const vase_pages& c, const void* q, int64_t q_stride
   a.out = out;
   a.lse = lse;
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = plan.bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.off_ml) : nullptr;
-  a.sums = plan.shares ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + plan.off_sums) : nullptr;
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.off_ml);
+  a.sums = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + plan.off_sums);
   a.n_tile = plan.n_tile;
   a.n_split = plan.n_split;
   a.keys = plan.keys;

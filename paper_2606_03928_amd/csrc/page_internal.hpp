@@ -71,12 +71,13 @@ __device__ __forceinline__ int find_slot(int S, int t, F f) {
 
 // page_attn.hip
 struct PageAttnPlan {
-  bool few;                // 16 rows to a workgroup; else 128
-  bool by_slot;            // few: max_new * G <= 16, a slot is one row tile
+  bool few;                // row tiles of 16 rows
+  bool by_slot;            // and a slot has one at most (max_new * G <= 16)
   int n_tile;              // row tiles of the batch, at most
   int n_split, keys;       // few: key ranges and their length
   int shares;              // else: workgroups among which the work is shared out, or 0
-  size_t off_ml, off_sums, bytes;   // workspace: partial outputs, their maxima and sums, ...
+  // workspace: partial outputs, their maxima and sums, the sums of the row tiles' key tiles
+  size_t off_ml, off_sums, bytes;
 };
 PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int max_len);
 hipError_t launch_page_attn(const vase_pages& c, const void* q, int64_t q_stride, const int32_t* cu,

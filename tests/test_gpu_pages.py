@@ -136,7 +136,7 @@ def test_attn(gpu_lib, shape, causal, dtype):
 @pytest.mark.parametrize("max_len", [1, 700, 2900, None])
 def test_attn_over_ranges_of_a_long_cache(gpu_lib, new, max_len, dtype):
     # few rows over long slots: the keys are split, whatever max_len says of the longest
-    c = make([2900, 1025, 70], 2, 64, 128, dtype, seed=3)
+    c = make([2900, 1025, 70], 2, 64, 128, dtype, M=50, seed=3)
     T = sum(new)
     q = queries(T, 8, 128, dtype, 4)
     lse = torch.empty((T, 8), device=DEV)
@@ -186,6 +186,93 @@ def test_attn_keeps_unseen_rows_out(gpu_lib, value, n, dtype):
     assert not torch.isfinite(got[-1, 2:, 77]).any()
     keep = torch.arange(128, device=DEV) != 77
     assert torch.equal(got[-1][:, keep], want[-1][:, keep])
+
+
+WIDE_TABLE = 1 << 20    # rows of a slot that a table may have: with it even a small batch is not a small call
+TILES = [  # page, d, H, G, lengths, new, rows of a slot at most
+    (16, 128, 2, 4, [1, 17, 300, 64], [1, 1, 40, 3], WIDE_TABLE),
+    (48, 64, 2, 3, [200, 7, 129], [77, 7, 1], WIDE_TABLE),
+    (64, 128, 1, 5, [257, 64, 500, 0], [130, 64, 0, 2], WIDE_TABLE),
+    (176, 128, 3, 2, [2500, 176, 1352], [170, 1, 176], WIDE_TABLE),
+    (128, 64, 2, 16, [2300, 128, 0], [1, 40, 0], WIDE_TABLE),
+    (16, 128, 1, 7, [90, 1, 31, 16, 47, 64, 5], [64, 1, 2, 16, 1, 0, 5], WIDE_TABLE),
+    (32, 64, 4, 1, [3000], [300], 0),                                     # workgroups with a part of a tile
+    (16, 128, 8, 4, [40 + 7 * i for i in range(40)], [1 + i for i in range(40)], WIDE_TABLE),   # with many tiles
+    (16, 64, 3, 2, [i % 19 for i in range(150)], [1 + i % 60 for i in range(150)], WIDE_TABLE),
+    (16, 64, 1, 2, [9 + i % 7 for i in range(1100)], [40] + [i % 3 for i in range(1099)], WIDE_TABLE),
+    (16, 128, 40, 4, [150, 1, 33], [130, 1, 33], 0),                      # a workgroup to each tile
+    (64, 64, 72, 3, [170, 64, 0, 200], [100, 9, 2, 200], 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", TILES, ids=lambda s: "d%d-H%d-G%d-S%d" % (s[1:4] + (len(s[4]),)))
+def test_attn_of_many_rows(gpu_lib, shape, causal, dtype):
+    page, d, H, G, lengths, new, most = shape
+    c = make(lengths, H, page, d, dtype, M=most // page or None, seed=20, gap=64)
+    T = sum(new)
+    q = queries(T + 3, H * G, d, dtype, 21, wide=H)
+    out = torch.full((T + 3, H * G, d), 7.0, dtype=dtype, device=DEV)
+    lse = torch.full((T + 3, H * G), 7.0, device=DEV)
+    ws = torch.full((c.attn_workspace_bytes(T + 3, G, max(new)) + 64,), 255, dtype=torch.uint8, device=DEV)
+    c.attn(q, ints(cumulative(new)), max(new), causal=causal, out=out, lse=lse, ws=ws)
+    torch.cuda.synchronize()
+    check_attn(c, q, new, out, lse, causal)
+    assert (out[T:] == 7).all() and (lse[T:] == 7).all()      # tokens of no slot
+    assert (ws[-64:] == 255).all() and int(c.status) == 0
+    again = torch.empty_like(out)
+    c.attn(q, ints(cumulative(new)), max(new), causal=causal, out=again, ws=ws.zero_())
+    assert torch.equal(again[:T], out[:T])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,M", [(2, WIDE_TABLE // 16), (40, 64)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_attn_of_many_rows_keeps_unseen_rows_out(gpu_lib, value, H, M, dtype):
+    n, L = 150, 330
+    c = make([L], H, 16, 128, dtype, M=M, seed=22)
+    q = queries(n, 2 * H, 128, dtype, 23)
+    cu = ints([0, n])
+    want = c.attn(q, cu, n)
+    keep = torch.arange(128, device=DEV) != 77
+    for x in (c.k, c.v):
+        for back in (1, 70):             # the last token's row; one of a tile that many rows see in part
+            at = (int(c.table[0, (L - back) // 16]), 1, (L - back) % 16, 77)
+            old = x[at].clone()
+            x[at] = value
+            got = c.attn(q, cu, n)
+            x[at] = old
+            assert torch.equal(got[:n - back], want[:n - back])           # rows that do not see it
+            assert torch.equal(got[:, :2], want[:, :2]) and torch.equal(got[:, 4:], want[:, 4:])
+            if x is c.v:
+                assert not torch.isfinite(got[n - back:, 2:4, 77]).any()
+                assert torch.equal(got[:, 2:4][..., keep], want[:, 2:4][..., keep])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attn_of_many_rows_at_the_edges(gpu_lib, dtype):
+    # scores of +-10^4, and a slot that has fewer rows than tokens
+    c = make([1700, 5], 1, 32, 64, dtype, M=WIDE_TABLE // 32, seed=24)
+    c.k.mul_(100)
+    q = queries(400, 2, 64, dtype, 25) * 10
+    lse = torch.empty((400, 2), device=DEV)
+    out = c.attn(q, ints([0, 340, 400]), 340, lse=lse)
+    check_attn(c, q, [340, 60], out, lse)
+    assert (out[340:395] == 0).all() and torch.isneginf(lse[340:395]).all()
+    # offsets that fall or leave the batch, and bad pages, read and write nothing outside
+    for cu in ([0, 400, 20], [390, 10, 400], [-5, 99, 9999], [400, 400, 400], [300, 300, 400]):
+        c.attn(q, ints(cu), 400, out=out)
+    small = make([1700, 5], 1, 32, 64, dtype, seed=24)
+    small.k.mul_(100)
+    for cu in ([0, 400, 20], [390, 10, 400], [-5, 99, 9999], [400, 400, 400], [300, 300, 400]):
+        small.attn(q, ints(cu), 400, max_len=64, out=out)
+    torch.cuda.synchronize()
+    assert int(c.status) == 0
+    c.table[0, 3], c.table[0, 40] = -1, c.n_pages
+    got = c.attn(q, ints([0, 340, 400]), 340)
+    assert int(c.status) == pages.STATUS_PAGE_BAD
+    check_attn(c, q, [340, 60], got, slots=[1])
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
