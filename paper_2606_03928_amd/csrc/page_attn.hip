@@ -8,11 +8,11 @@
 // (bf16: ds_read_b64_tr_b16) in the same order of keys.  No probability moves
 // between lanes or through LDS.
 //
-// Two kernels: page_tile_kernel takes 128 query rows to a workgroup and is bound by its
-// MFMAs and exponentials; page_few_kernel takes 16 (a token of decoding) and is bound by
-// the K and V rows it reads.  Where workgroups would be too few or too uneven to fill the
-// chip, the keys are split, and partial (m, l, O) are joined in the order of their keys by a
-// launch behind: ranges of one length (few), equal shares of all tiles (tile).
+// Many rows are bound by MFMAs and exponentials: page_wide_kernel takes 256 (bf16) and
+// page_tile_kernel 128 (fp32) to a workgroup.  Few (tokens of decoding) are bound by the K
+// and V rows that they read: page_few_kernel takes 16.  Where workgroups would be too few or too
+// uneven to fill the chip, the keys are split, and partial (m, l, O) are joined in the order
+// of their keys by a launch behind: ranges of one length (few), equal shares of all tiles.
 //
 // Masked keys take p = 0 by a select on the score, and V rows behind the slot's end are
 // zeroed where they are staged.  A later token's V row may hold an infinity or a NaN, which
@@ -82,11 +82,13 @@ struct Span {
   }
 };
 
-// Row tiles of R rows: those of slot s begin at number floor(cu[s] G / R) + s, which leaves
-// room for all of its rows, so that a tile's slot is found in cu alone.
+// Row tiles of R rows: those of slot s begin at number floor(cu[s] G / R) + min(s, cu[s]).  No more
+// than min(s, cu[s]) slots before it have tokens, so there is room for a last tile of each, a
+// tile's slot is found in cu alone, and slots without tokens behind the last add no tiles.
 template <int R>
 __device__ __forceinline__ int first_tile(const AttnArgs& a, const int32_t* cu, int s) {
-  return (int)((int64_t)min(max(cu[s], 0), a.T) * a.G / R) + s;
+  const int c = min(max(cu[s], 0), a.T);
+  return (int)((int64_t)c * a.G / R) + min(s, c);
 }
 template <int R>
 __device__ __forceinline__ int first_tile(const AttnArgs& a, int s) {
@@ -227,9 +229,10 @@ __device__ __forceinline__ pbf16x8 read_vt(const u4* base, int byte0, int byte1)
 }
 
 // ---------------------------------------------------------------------------
-// The tile kernel.  A wave keeps 32 query rows (one per lane column) and their O^T in
-// registers; K and V tiles of BN keys pass through two LDS buffers, the next tile's
-// rows on their way to registers while this one is used.
+// The tile kernel (fp32).  A wave keeps 32 query rows (one per lane column) and their O^T in
+// registers; K and V tiles of 32 keys pass through two LDS buffers, the next tile's
+// rows on their way to registers while this one is used.  8 slots of 192 tokens over 2100 rows, 4
+// heads to each of 8 KV heads of 128: 583 us, 86 TFLOP/s of the 153 that a large fp32 product reaches.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct Tile {
@@ -256,8 +259,10 @@ struct Tile {
 
 // Shares: the (head, row tile, key tile) triples in that order, cut into equal parts for at most
 // a.shares workgroups and none below kLeastShare triples.  A row tile's beginning and end (Q, the
-// first loads, its output: 9 us) count as kSetup triples before its first.  What a workgroup
-// cannot finish of a row tile (its first and last at most) it leaves as a partial.
+// first loads, its output: 11 us, where a key tile takes 1.9) count as kSetup triples before
+// its first: with none a fresh prompt's short tiles made some parts twice as long as others
+// (3200 tokens: 202 us, with 6 under 120).  What a workgroup cannot finish of a row tile (its
+// first and last at most) it leaves as a partial.
 constexpr int kMaxTiles = 1023;    // row tiles whose sums a workgroup keeps
 constexpr int kLeastShare = 4;
 constexpr int kSetup = 6;
@@ -272,7 +277,7 @@ struct Shares {
   __device__ __forceinline__ int of(int64_t x) const { return (int)((x * n + n - 1) / total); }
 };
 
-// cu, of which a slot is searched for often: S < n_tile <= kMaxTiles
+// cu, in which a slot is searched for often: S <= kMaxTiles
 __device__ __forceinline__ void keep_cu(const AttnArgs& a, int32_t* s_cu) {
   for (int x = threadIdx.x; x <= a.c.S; x += kBlock) s_cu[x] = a.cu[x];
 }
@@ -550,7 +555,10 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
 // they do within one, so a wave has its SIMD to itself and its steps of 32 keys overlap:
 // step t's exponentials run beside the scores of step t + 1 and the V product of step t - 1.
 // Maxima that grow by less than 2^8 leave the reference alone (a probability is then at most
-// 2^8, its rounding to bf16 relative as before).
+// 2^8, its rounding to bf16 relative as before).  4 slots of 2048 tokens over 4096 to 8448 rows, 5
+// heads to each of 8 KV heads of 128: 980 to 1110 us by the card's clock, 1.05 to 0.93
+// PFLOP/s, where a product of 8192^3 reaches 1.15; with 128 rows to a workgroup and two to a
+// CU 1200 to 1390.  What is left is the power limit: the clock falls to 1.9 GHz under it.
 // ---------------------------------------------------------------------------
 constexpr int kWideRows = 64 * kWaves;
 
@@ -959,6 +967,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
   constexpr int U = 4;                                                    // partials in flight
   const int tile = (int)(blockIdx.x / kPer) % a.n_tile, h = (int)(blockIdx.x / kPer) / a.n_tile;
   const int per_head = a.sums[a.n_tile], sum0 = a.sums[tile], sum1 = a.sums[tile + 1];
+  const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<R>(a, s); }));   // while those come
   if (sum1 <= sum0) return;
   const Shares sh(a, per_head);
   const int64_t x0 = (int64_t)h * per_head + sum0, x1 = (int64_t)h * per_head + sum1;
@@ -967,29 +976,28 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
   // the first part's partial is that of its last row tile if it began before this one; the others
   // begin in it
   const int64_t place0 = ((int64_t)first * 2 + (sh.begin(first) < x0)) * R;
-  const Span sp(a, find_slot(a.c.S, tile, [&](int s) { return first_tile<R>(a, s); }));
   const int r0 = (tile - first_tile<R>(a, sp.s)) * R;
   const int d0 = threadIdx.x % TPR * 4, r = (int)(blockIdx.x % kPer) * RPB + threadIdx.x / TPR;
   if (r0 < 0 || r0 + r >= sp.n * a.G) return;
   auto place = [&](int i) { return (i == first ? place0 : (int64_t)i * 2 * R) + r; };
-  auto ml = [&](int i) { return *reinterpret_cast<const float2*>(a.part_ml + place(i) * 2); };
-  float top = -INFINITY;
-  for (int i = first; i <= last; i += U) {
-    float m[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) m[u] = ml(min(i + u, last)).x;
-#pragma unroll
-    for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
-  }
-  float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
   for (int i = first; i <= last; i += U) {
     float2 y[U];
     float4 z[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      y[u] = ml(min(i + u, last));
-      z[u] = *reinterpret_cast<const float4*>(a.part_o + place(min(i + u, last)) * D + d0);
+      const int64_t at = place(min(i + u, last));
+      y[u] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      z[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + d0);
     }
+    float now = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) now = fmaxf(now, y[u].x);
+    const float old = top == -INFINITY ? 0.f : exp2_(top - now);
+    top = now;
+    l *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= old;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u > last) break;
@@ -1015,6 +1023,8 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
 // fourth tile of 32 keys (fp32: 16).  K rows go from memory into A operands as they are, V rows
 // through a piece of LDS that the wave has alone; the waves' states are joined at the
 // end.  The next tile's rows are loaded as soon as this one's have left their registers.
+// 64 slots of 2000 to 8320 rows, one token, 8 heads to each of 8 KV heads of 128: 250 us, 5.4
+// TB/s (a large copy reaches 5 to 6).
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct Few {
@@ -1304,14 +1314,20 @@ PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int 
   const int slots = std::min(c.S, T);          // that can have tokens
   const int64_t most = (int64_t)max_new * G;   // rows of a slot
   const double reads = (double)((int64_t)T * G / kFewRows + slots) * c.H * max_len * c.d;   // of K by 16-row tiles
-  p.by_slot = most <= kFewRows;
+  // 16-row tiles read K and V once each, larger ones begin late (13 us, with shares 25) and work
+  // on rows that are not there.  8 slots over 4200 rows, 8 KV heads of 128, us of 16-row tiles and of
+  // larger: 32 rows to a slot 53 and 59, 64 rows 88 and 60; fp32 32 rows 104 and 217, 64 rows 178
+  // and 221, 128 rows (more) and 236.  Small calls: 1 slot over 4224 rows, 64 query rows (22 M
+  // elements read) 26 and 34, 128 (39 M) 36 and 36; 256 over 1000 rows (17 M) 19 and 36.
+  p.by_slot = most <= kFewRows && c.S <= T;
   p.few = most <= (wide ? 32 : 64) || reads <= 1 << 25;
   p.n_split = 1;
   p.keys = max_len;
   if (p.few) {
     const size_t rows = (size_t)T * c.H * G;
-    p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + c.S;
-    // at least 256 keys to a range, up to kMaxSplit ranges
+    p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + slots;
+    // 8 workgroups to a CU, at least 256 keys to a range (512 and 1024 took as long), up to
+    // kMaxSplit ranges
     const int64_t wgs = (p.by_slot ? slots : (int64_t)T * G / kFewRows + 1) * c.H;
     int64_t s = 2048 / wgs + 1;
     if (s > kMaxSplit) s = kMaxSplit;
@@ -1326,11 +1342,16 @@ PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int 
     return p;
   }
   const int R = wide ? kWideRows : kTileRows;
-  p.n_tile = (int)((int64_t)T * G / R) + c.S;
+  p.n_tile = (int)((int64_t)T * G / R) + slots;
   const int shares = 256 * (wide ? 1 : tile_waves(c.d));   // workgroups that run at once
   const int64_t tiles = ((int64_t)T * G / R + 1) * c.H, most_tiles = max_new <= max_len / 2 ? shares * 3 / 2 : shares;
-  // the sums of 32-key tiles stay in 32 bits
-  if (tiles <= most_tiles && p.n_tile <= kMaxTiles && max_len > 1024 &&
+  // Where a second round of workgroups would run half empty or there is no full first one: us
+  // shared (with the launch behind) and not, row tiles of about as many keys (8 slots, histories of
+  // 3000 to 8000 rows): 328 row tiles 168 and 183, 264 and 320; 392 191 and 188, 311 and 329; 456 220
+  // and 198, 358 and 375.  A fresh prompt's run from long to short and fill the gaps: 208
+  // row tiles 62 and 54, 300 94 and 78, but 144 50 and 63.
+  // The sums of 32-key tiles stay in 32 bits.
+  if (tiles <= most_tiles && p.n_tile <= kMaxTiles && c.S <= kMaxTiles && max_len > 1024 &&
       (int64_t)p.n_tile * (c.M * c.page / 32 + 1 + kSetup) <= 0x7fffffff) {
     p.shares = shares;
     const size_t part = (size_t)p.shares * 2 * R;

@@ -200,6 +200,8 @@ TILES = [  # page, d, H, G, lengths, new, rows of a slot at most
     (16, 128, 8, 4, [40 + 7 * i for i in range(40)], [1 + i for i in range(40)], WIDE_TABLE),   # with many tiles
     (16, 64, 3, 2, [i % 19 for i in range(150)], [1 + i % 60 for i in range(150)], WIDE_TABLE),
     (16, 64, 1, 2, [9 + i % 7 for i in range(1100)], [40] + [i % 3 for i in range(1099)], WIDE_TABLE),
+    (16, 64, 2, 4, [3 + i % 50 for i in range(900)], [0] * 300 + [100] + [0] * 598 + [17], WIDE_TABLE),
+    (16, 64, 3, 4, [3 + i % 50 for i in range(900)], [0] * 7 + [1] + [0] * 700 + [4] + [0] * 190 + [2], 0),
     (16, 128, 40, 4, [150, 1, 33], [130, 1, 33], 0),                      # a workgroup to each tile
     (64, 64, 72, 3, [170, 64, 0, 200], [100, 9, 2, 200], 0),
 ]
