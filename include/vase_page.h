@@ -110,8 +110,8 @@ size_t vase_page_workspace_bytes(int op, const vase_pages* c, int T, int G, int 
  * unspecified), len[s] outside [0, M * page] (taken as the nearest of both), or max_new
  * exceeded.
  * Errors: VASE_ERR_INVALID_ARG (null or unaligned pointer, sizes out of range),
- *         VASE_ERR_DTYPE, VASE_ERR_WORKSPACE, VASE_ERR_UNSUPPORTED (more than 2^31 - 1
- *         workgroups), VASE_ERR_HIP.
+ *         VASE_ERR_DTYPE, VASE_ERR_WORKSPACE, VASE_ERR_UNSUPPORTED (2^24 or more
+ *         workgroups, or 2^31 or more query rows), VASE_ERR_HIP.
  */
 int vase_page_attn(const vase_pages* c, const void* q, int64_t q_stride, const int32_t* cu, int T,
                    int G, int max_new, int max_len, int causal, void* out, float* lse, void* ws,

@@ -8,6 +8,8 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 
 constexpr int kMaxHeads = 65536, kMaxSlots = 65536, kMaxPage = 65536, kMaxTokens = 1 << 24;
 
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;   // of 256 threads: a launch has less than 2^32
+
 // strides in elements: whole 16-byte pieces
 bool whole_pieces(int64_t stride, int dtype) { return stride % (dtype == VASE_BF16 ? 8 : 4) == 0; }
 
@@ -75,7 +77,7 @@ int vase_page_attn(const vase_pages* c, const void* q, int64_t q_stride, const i
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(cu, 4))
     return VASE_ERR_INVALID_ARG;
   const vase::PageAttnPlan plan = vase::page_attn_plan(*c, T, G, max_new, max_len);
-  if ((int64_t)plan.n_tile * c->H > 0x7fffffffLL / plan.n_split || (int64_t)T * c->H * G > 0x7fffffffLL)
+  if ((int64_t)plan.n_tile * c->H > kMaxBlocks / plan.n_split || (int64_t)T * c->H * G > 0x7fffffffLL)
     return VASE_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || ws_bytes < plan.bytes || !aligned(ws, 16))) return VASE_ERR_WORKSPACE;
   return hip_status(vase::launch_page_attn(*c, q, q_stride, cu, T, G, causal, out, lse, ws, plan,

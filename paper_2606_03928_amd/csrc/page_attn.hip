@@ -76,6 +76,10 @@ struct Span {
     L = slot_len(a.c, s);
   }
   __device__ __forceinline__ Span(const AttnArgs& a, int slot) : Span(a, a.cu, slot) {}
+  // for a workgroup that has rows of the slot: a length that was out of range
+  __device__ __forceinline__ void check(const AttnArgs& a) const {
+    if (threadIdx.x == 0 && a.status && a.c.len[s] != L) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
+  }
   // rows that token i sees
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {
     return a.causal ? max(L - n + i + 1, 0) : L;
@@ -403,6 +407,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
     const Span sp(a, cu, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, cu, s); }));
     const int rows = sp.n * a.G, r0 = (tile - first_tile<kTileRows>(a, cu, sp.s)) * kTileRows;
     if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
+    sp.check(a);
 
     // the keys that this lane's row sees
     const int lim = sp.sees(a, min(r0 + 32 * wave + l32, rows - 1) / a.G);
@@ -597,6 +602,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     const Span sp(a, cu, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, cu, s); }));
     const int rows = sp.n * a.G, r0 = (sg.tile - first_tile<kWideRows>(a, cu, sp.s)) * kWideRows;
     if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
+    sp.check(a);
 
     // the keys that this lane's two rows see
     int lim[2];
@@ -1067,6 +1073,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   }
   const int rows = min(sp.n * a.G - r0, kFewRows);   // of this tile
   if (r0 < 0 || rows <= 0) return;   // none; r0 < 0: cu that falls
+  sp.check(a);
   const int row = r0 + min(l16, rows - 1);
   const int tok = row / a.G, g = row - tok * a.G;
   const int lim = sp.sees(a, tok);

@@ -189,8 +189,9 @@ class PageCache:
             if ws is None:
                 ws = self._state_ws = torch.empty(self.state_workspace_bytes(), dtype=torch.uint8,
                                                   device=self.device)
-            if stream is not None:
-                ws.record_stream(stream)
+                self._state_home = _stream_ptr(self.device, None)
+            if _stream_ptr(self.device, stream) != self._state_home:
+                ws.record_stream(stream if stream is not None else torch.cuda.current_stream(self.device))
             return ws.data_ptr(), ws.numel(), ws
         return self._ws(ws, self._bytes(op), stream)
 

@@ -347,6 +347,54 @@ def test_attn_flags_bad_pages_and_stays_inside(gpu_lib):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("M,n", [(8, 1), (8, 30), (WIDE_TABLE // 16, 50)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attn_flags_lengths_out_of_range(gpu_lib, dtype, M, n):
+    c = make([60, 60, 60], 1, 16, 64, dtype, M=M, seed=26, garbage=0.0)
+    q = queries(3 * n, 2, 64, dtype, 27)
+    cu = ints([0, n, 2 * n, 3 * n])
+    want = c.attn(q, cu, n)
+    assert int(c.status) == 0
+    for bad in (-1, -2 ** 31, M * 16 + 1, 2 ** 31 - 1):
+        if bad > 0 and M > 8:
+            continue                                 # 2^20 rows of page 0: nothing to learn
+        c.length[1] = bad
+        got = c.attn(q, cu, n)
+        assert torch.equal(got[:n], want[:n]) and torch.equal(got[2 * n:], want[2 * n:])
+        assert int(c.status) == pages.STATUS_PAGE_BAD
+        if bad < 0:
+            assert (got[n:2 * n] == 0).all()
+        c.status.zero_()
+
+
+def test_state_workspace_on_other_streams(gpu_lib):
+    """A cache's own workspace is made on one stream and used on others, by name or as the
+    current one; what is allocated where it lay must not run ahead of them."""
+    want = None
+    for by_name in (None, False, True):
+        c = make([100, 37, 5], 2, 16, 64, F32, M=20, extra=40, seed=28)
+        c.resize(ints([90, 37, 5]))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        more = ints([200, 60, 5])
+        torch.cuda.synchronize()
+        if by_name is None:
+            c.resize(more)
+        elif by_name:
+            c.resize(more, stream=side)
+        else:
+            with torch.cuda.stream(side):
+                c.resize(more)
+        state = (c.table, c.length, c.ref)
+        size = c.state_workspace_bytes()
+        del c
+        torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        got = [x.tolist() for x in state]
+        assert want is None or got == want
+        want = got
+
+
 # --- state --------------------------------------------------------------------------------
 
 

@@ -92,6 +92,16 @@ def test_attn_refuses(lib, kw, code):
         assert attn(lib, None, **kw) == code
 
 
+def test_attn_refuses_more_workgroups_than_a_launch_takes(lib):
+    # a workgroup of 256 threads to each slot and head: 2^24 of them would be 2^32 threads
+    T, H = 1 << 16, 256
+    c = cache(S=T, H=H, page_stride=H * 64 * 128)
+    assert attn(lib, c, T=T, G=1, max_new=1, stride=H * 128, wsb=1 << 62) == vase.ERR_UNSUPPORTED
+    # 2^31 query rows
+    c = cache(S=128, H=1 << 12, page_stride=(1 << 12) * 64 * 128)
+    assert attn(lib, c, T=1 << 15, G=16, max_new=1 << 15, stride=(1 << 16) * 128, wsb=1 << 62) == vase.ERR_UNSUPPORTED
+
+
 def test_the_others_refuse(lib):
     c = cache()
     r = ctypes.byref(c)
