@@ -133,6 +133,10 @@ struct GroupBases {
 __device__ __forceinline__ u4 load_at(uint64_t address, uint32_t offset) {
   return *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(address) + offset);
 }
+// the same of what is not read again soon
+__device__ __forceinline__ u4 load_once_at(uint64_t address, uint32_t offset) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u4*>(reinterpret_cast<const char*>(address) + offset));
+}
 // from an address in the K pool to the same row's in the V pool
 __device__ __forceinline__ uint64_t to_v(const PageView& c) {
   return reinterpret_cast<uint64_t>(c.v) - reinterpret_cast<uint64_t>(c.k);
@@ -1029,7 +1033,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
 // fourth tile of 32 keys (fp32: 16).  K rows go from memory into A operands as they are, V rows
 // through a piece of LDS that the wave has alone; the waves' states are joined at the
 // end.  The next tile's rows are loaded as soon as this one's have left their registers.
-// 64 slots of 2000 to 8320 rows, one token, 8 heads to each of 8 KV heads of 128: 250 us, 5.4
+// 64 slots of 2000 to 8320 rows, one token, 8 heads to each of 8 KV heads of 128: 234 us, 5.8
 // TB/s (a large copy reaches 5 to 6).
 // ---------------------------------------------------------------------------
 template <typename T, int D>
@@ -1050,7 +1054,7 @@ struct Few {
   }
 };
 
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   using S = Few<T, D>;
   constexpr int BN = S::BN, NS = S::NS, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
@@ -1106,7 +1110,11 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) rk[n][ks] = load_at(at, (l16 * PPR + 4 * ks + quad) * 16);
 #pragma unroll
-      for (int i = 0; i < NP / NS; ++i) rv[n * (NP / NS) + i] = load_at(at + to_v(a.c), (i * kWave + lane) * 16);
+      for (int i = 0; i < NP / NS; ++i) {
+        const uint64_t av = at + to_v(a.c);
+        const uint32_t offset = (i * kWave + lane) * 16;
+        rv[n * (NP / NS) + i] = ONCE ? load_once_at(av, offset) : load_at(av, offset);
+      }
     }
   };
   u4* tv = s_v[wave];
@@ -1292,7 +1300,9 @@ hipError_t launch_td(const AttnArgs& a, const PageAttnPlan& pl, hipStream_t stre
   constexpr int R = kWide ? kWideRows : kTileRows;
   const dim3 block(kBlock);
   if (pl.few) {
-    hipLaunchKernelGGL((page_few_kernel<T, D>), dim3((unsigned)(a.n_tile * a.c.H * a.n_split)), block, 0, stream, a);
+    const dim3 grid((unsigned)(a.n_tile * a.c.H * a.n_split));
+    if (pl.once) hipLaunchKernelGGL((page_few_kernel<T, D, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((page_few_kernel<T, D, false>), grid, block, 0, stream, a);
     // a wave per row
     if (a.n_split > 1)
       hipLaunchKernelGGL((page_combine_kernel<T, D>), dim3((unsigned)(((int64_t)a.T * a.HG + kWaves - 1) / kWaves)),
@@ -1333,6 +1343,11 @@ PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int 
   if (p.few) {
     const size_t rows = (size_t)T * c.H * G;
     p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + slots;
+    // V rows past the caches where each is read once, from 2^17 of them on (bf16, d 128: 32 MB): us
+    // with plain loads and so, 64 slots of 2000 to 8320 rows 251 and 234, 256 of 500 to 4224 441 and
+    // 419, 8 of 4200 25 and 25; one of 4224, which stays in the caches, 8.3 and 9.3.
+    // Not K rows: an operand load takes 64 bytes of each, half of a line (256 slots 492).
+    p.once = p.by_slot && (int64_t)slots * c.H * max_len >= 1 << 17;
     // 8 workgroups to a CU, at least 256 keys to a range (512 and 1024 took as long), up to
     // kMaxSplit ranges
     const int64_t wgs = (p.by_slot ? slots : (int64_t)T * G / kFewRows + 1) * c.H;

@@ -73,6 +73,7 @@ __device__ __forceinline__ int find_slot(int S, int t, F f) {
 struct PageAttnPlan {
   bool few;                // row tiles of 16 rows
   bool by_slot;            // and a slot has one at most (max_new * G <= 16)
+  bool once;               // V rows are read once, more of them than the caches keep
   int n_tile;              // row tiles of the batch, at most
   int n_split, keys;       // few: key ranges and their length
   int shares;              // else: workgroups among which the work is shared out, or 0
