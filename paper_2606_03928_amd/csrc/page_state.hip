@@ -358,8 +358,7 @@ __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView 
   int n = 0;
   for (int base = 0; base < c.S; base += kPlanBlock) {
     const int s = base + threadIdx.x;
-    const int m = s < c.S ? map[s] : -1;
-    const int L = m >= 0 ? c.len[s] : 0;
+    const int m = s < c.S ? map[s] : -1, L = s < c.S ? c.len[s] : 0;
     const bool ok = m >= 0 && m < n_map && L >= K && L <= c.M * c.page;
     bad |= m >= 0 && !ok;
     long long all;
@@ -372,12 +371,22 @@ __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView 
     n += (int)all;
   }
   bad = __syncthreads_or(bad);   // also: the lists and s_most are written
-  const int most = s_most, kept = pages_for(c, K);
+  const int64_t items = (int64_t)n * c.H;
+  if (items < kFewItems) {
+    for (int i = threadIdx.x; i < items; i += kPlanBlock) w.ticket[i * kTicketGap] = 0;
+    for (int64_t i = threadIdx.x; i < items * ((K + chunk - 1) / chunk); i += kPlanBlock) w.said[i] = 0;
+  }
+  const int most = max(s_most, 1), kept = pages_for(c, K);
   const int64_t pairs = bad ? 0 : (int64_t)n * most;
   long long need = 0;
-  for (int64_t base = 0; base < pairs; base += kPlanBlock) {
+  int e = threadIdx.x / most, j = threadIdx.x % most;   // of pair i
+  const int e_step = kPlanBlock / most, j_step = kPlanBlock % most;
+  for (int64_t base = 0; base < pairs; base += kPlanBlock, e += e_step, j += j_step) {
     const int64_t i = base + threadIdx.x;
-    const int e = (int)(i / most), j = (int)(i % most);
+    if (j >= most) {
+      j -= most;
+      ++e;
+    }
     bool shared = false;
     if (i < pairs && j < pages_for(c, w.len[e])) {
       const int p = c.table[(int64_t)w.slot[e] * c.M + j];
@@ -394,11 +403,6 @@ __global__ __launch_bounds__(kPlanBlock) void page_compact_plan_kernel(PageView 
   bad = __syncthreads_or(bad);
   bool full = need > c.n_pages;
   if (!bad && !full && need > 0) full = list_free(c.ref, c.n_pages, (int)need, first_look, w.free, s_count) < need;
-  const int64_t items = (int64_t)n * c.H;
-  if (items < kFewItems) {
-    for (int i = threadIdx.x; i < items; i += kPlanBlock) w.ticket[i * kTicketGap] = 0;
-    for (int64_t i = threadIdx.x; i < items * ((K + chunk - 1) / chunk); i += kPlanBlock) w.said[i] = 0;
-  }
   if (threadIdx.x == 0) {
     w.head[0] = !bad && !full;
     w.head[1] = n;
