@@ -347,6 +347,52 @@ def test_attn_flags_bad_pages_and_stays_inside(gpu_lib):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("n", [1, 17])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attn_over_a_million_rows(gpu_lib, dtype, n):
+    L = 1_050_037
+    c = make([70, L], 1, 1024, 64, dtype, seed=29, garbage=0.0, extra=1)
+    q = queries(n + 1, 4, 64, dtype, 30)
+    lse = torch.empty((n + 1, 4), device=DEV)
+    out = c.attn(q, ints([0, 1, n + 1]), n, lse=lse)
+    check_attn(c, q, [1, n], out, lse)
+    assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,H", [(WIDE_TABLE // 16, 2), (40, 40)])
+def test_attn_of_many_rows_captured(gpu_lib, M, H, dtype):
+    """A chunk's attention captured once and replayed over other lengths, offsets and queries,
+    with eager calls between: what the host said at capture are upper bounds alone."""
+    T, G = 200, 2
+    c = make([600, 333, 90], H, 16, 128, dtype, M=M, seed=31, garbage=0.0)
+    q = queries(T, H * G, 128, dtype, 32)
+    cu = ints([0, 120, 121, 200])
+    out, lse = torch.zeros((T, H * G, 128), dtype=dtype, device=DEV), torch.zeros((T, H * G), device=DEV)
+    ws = torch.empty(max(c.attn_workspace_bytes(T, G, 150), 16), dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.attn(q, cu, 150, out=out, lse=lse, ws=ws)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            c.attn(q, cu, 150, out=out, lse=lse, ws=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    for new, length in (([120, 1, 79], [600, 333, 90]), ([50, 150, 0], [599, 150, 0]), ([1, 1, 1], [17, 333, 1]),
+                        ([0, 130, 70], [600, 140, 64]), ([120, 1, 79], [600, 333, 90])):
+        cu.copy_(ints(cumulative(new)))
+        c.length.copy_(ints(length))
+        q.normal_()
+        out.fill_(7), lse.fill_(7)
+        g.replay()
+        check_attn(c, q, new, out, lse)
+        n = sum(new)
+        assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+        eager = c.attn(q, cu, 150, ws=ws)
+        assert torch.equal(eager[:n], out[:n])
+    assert int(c.status) == 0
+
+
 @pytest.mark.parametrize("M,n", [(8, 1), (8, 30), (WIDE_TABLE // 16, 50)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attn_flags_lengths_out_of_range(gpu_lib, dtype, M, n):
