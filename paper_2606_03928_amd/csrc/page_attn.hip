@@ -56,10 +56,10 @@ struct AttnArgs {
   int causal;
   void* out;
   float* lse;
-  // partials.  few: [range][T][HG] of D and of 2; tile: [workgroup][2][128] likewise
+  // partials.  few: [range][T][HG] of D and of 2; tile: [workgroup][2][its rows] likewise
   float *part_o, *part_ml;
-  int32_t* sums;           // tile, shares: [n_tile + 1], the sums of the row tiles' key tiles
-  int n_tile;              // few: row tiles of 16 rows; tile: of 128
+  int32_t* sums;           // tile, shares: [n_tile + 1], the sums of the row tiles' triples
+  int n_tile;              // row tiles, at most
   int n_split, keys;       // few: key ranges
   int by_slot;             // few: a slot's rows are one row tile
   int shares;              // tile: workgroups that share the work (0: one to a row tile and head)
