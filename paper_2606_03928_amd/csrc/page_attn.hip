@@ -67,6 +67,9 @@ struct AttnArgs {
   uint32_t* status;
 };
 
+// x, the same in all lanes, kept for the wave as a whole (what comes out of LDS is not by itself)
+__device__ __forceinline__ int of_wave(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // A slot's share of the batch, read as it stands but kept inside the caller's arrays.
 struct Span {
   int s, c0, n, L;   // slot, first token, tokens, rows
@@ -76,6 +79,14 @@ struct Span {
     L = slot_len(a.c, s);
   }
   __device__ __forceinline__ Span(const AttnArgs& a, int slot) : Span(a, a.cu, slot) {}
+  __device__ __forceinline__ Span of_all() const {   // where all lanes have the same
+    Span x = *this;
+    x.s = of_wave(s);
+    x.c0 = of_wave(c0);
+    x.n = of_wave(n);
+    x.L = of_wave(L);
+    return x;
+  }
   // for a workgroup that has rows of the slot: a length that was out of range
   __device__ __forceinline__ void check(const AttnArgs& a) const {
     if (threadIdx.x == 0 && a.status && a.c.len[s] != L) atomicOr(a.status, VASE_STATUS_PAGE_BAD);
@@ -337,10 +348,14 @@ __device__ __forceinline__ bool share_out(const AttnArgs& a, uint32_t id, int32_
   __syncthreads();
   if (id == 0)
     for (int x = threadIdx.x; x <= a.n_tile; x += kBlock) a.sums[x] = s_sum[x];
-  const Shares sh(a, s_sum[a.n_tile]);
+  const Shares sh(a, of_wave(s_sum[a.n_tile]));
   if (sh.total == 0 || (int)id >= sh.n) return false;
-  next = sh.begin(id);
-  end = sh.begin(id + 1);
+  auto begin = [&](int i) {
+    const int64_t x = sh.begin(i);
+    return (int64_t)of_wave((int)(x >> 32)) << 32 | (uint32_t)of_wave((int)x);
+  };
+  next = begin(id);
+  end = begin(id + 1);
   return true;
 }
 
@@ -351,17 +366,17 @@ struct Segment {
 };
 __device__ __forceinline__ Segment next_segment(const AttnArgs& a, const int* s_sum, int64_t& next, int64_t end) {
   Segment g;
-  const int per_head = s_sum[a.n_tile];
-  g.h = (int)(next / per_head);
+  const int per_head = of_wave(s_sum[a.n_tile]);
+  g.h = of_wave((int)(next / per_head));
   const int at = (int)(next - (int64_t)g.h * per_head);
   int lo = 0, hi = a.n_tile;     // the last tile that begins at or before it, and is not empty
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (s_sum[mid] <= at) lo = mid;
+    if (of_wave(s_sum[mid]) <= at) lo = mid;
     else hi = mid;
   }
-  g.tile = __builtin_amdgcn_readfirstlane(lo);
-  const int first = at - s_sum[g.tile], all = s_sum[g.tile + 1] - s_sum[g.tile];
+  g.tile = lo;
+  const int sum = of_wave(s_sum[lo]), first = at - sum, all = of_wave(s_sum[lo + 1]) - sum;
   const int upto = (int)min((int64_t)all, first + (end - next));
   g.kt0 = max(first - kSetup, 0);
   g.kt1 = max(upto - kSetup, 0);   // none: another workgroup's
@@ -408,8 +423,8 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
     }
     const int tile = sg.tile, h = sg.h;
     const bool whole = sg.whole;
-    const Span sp(a, cu, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, cu, s); }));
-    const int rows = sp.n * a.G, r0 = (tile - first_tile<kTileRows>(a, cu, sp.s)) * kTileRows;
+    const Span sp = Span(a, cu, find_slot(a.c.S, tile, [&](int s) { return first_tile<kTileRows>(a, cu, s); })).of_all();
+    const int rows = sp.n * a.G, r0 = (tile - of_wave(first_tile<kTileRows>(a, cu, sp.s))) * kTileRows;
     if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
     sp.check(a);
 
@@ -582,9 +597,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
   __shared__ int32_t s_cu[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int s_wave[kWaves];
 
-  const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int l32 = lane % 32, half = lane / 32;
   const uint32_t id = xcd_logical_block(blockIdx.x, gridDim.x);
   const int32_t* cu = SHARES ? s_cu : a.cu;
   int64_t next = 0, end = 1;
@@ -593,6 +606,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
   }
 
   for (int seg = 0; next < end; ++seg) {
+    const int lane = lane_here(), l32 = lane % 32, half = lane / 32, tid = wave * kWave + lane;
     Segment sg;
     if constexpr (SHARES) {
       sg = next_segment(a, s_sum, next, end);
@@ -603,21 +617,21 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       next = end;
     }
     const int h = sg.h;
-    const Span sp(a, cu, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, cu, s); }));
-    const int rows = sp.n * a.G, r0 = (sg.tile - first_tile<kWideRows>(a, cu, sp.s)) * kWideRows;
+    const Span sp = Span(a, cu, find_slot(a.c.S, sg.tile, [&](int s) { return first_tile<kWideRows>(a, cu, s); })).of_all();
+    const int rows = sp.n * a.G, r0 = (sg.tile - of_wave(first_tile<kWideRows>(a, cu, sp.s))) * kWideRows;
     if (r0 < 0 || r0 >= rows) return;   // none; r0 < 0: cu that falls
     sp.check(a);
 
-    // the keys that this lane's two rows see
-    int lim[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) lim[c] = sp.sees(a, min(r0 + 64 * wave + 32 * c + l32, rows - 1) / a.G);
-    const int wave_lo = __builtin_amdgcn_readfirstlane(lim[0]);           // the wave's first row's
+    // the keys that this lane's two rows see; computed anew where they matter
+    auto lim = [&](int c) INLINE {
+      return sp.sees(a, min(r0 + 64 * wave + 32 * c + lane_here() % 32, rows - 1) / a.G);
+    };
+    const int wave_lo = sp.sees(a, min(r0 + 64 * wave, rows - 1) / a.G);   // the wave's first row's
     const int kb = sg.kt0 * BN;
     const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kWideRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
     const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
     const int steps = max((ke - kb + BN - 1) / BN, 0) * 2;   // whole tiles: what lies behind is masked
-    if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+    if (tid < D) s_bad[tid] = 0x7fffffff;
     __syncthreads();
 
     u4 qf[2][KS];
@@ -635,10 +649,11 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][c][i] = 0.f;
-    // a row's reference m (in score units), mc (in log2 units), what a score must pass for m to
-    // follow, and the sum l over this lane's keys
+    // a row's reference m (in score units), mc (in log2 units), and the sum l over this lane's
+    // keys; a score must pass m by more than slack for m to follow
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, alpha[2] = {1.f, 1.f};
-    float mc[2] = {0.f, 0.f}, pass[2] = {-INFINITY, -INFINITY};
+    float mc[2] = {0.f, 0.f};
+    const float slack = 8.f / a.scale_log2;
     bool grown = false;   // m has changed for the step in hand: O follows behind its V product
 
     GroupBases<PPR> bases;
@@ -655,11 +670,11 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     };
     auto load_v = [&](int i) INLINE { rv[i] = load_at(at_v[i], offset); };
     auto put_k = [&](int b, int i) INLINE {
-      const int x = i * kBlock + threadIdx.x;
+      const int x = i * kBlock + tid;
       s_k[b][S::k_at(x / PPR, x % PPR)] = rk[i];
     };
     auto put_v = [&](int b, int i) INLINE {
-      const int x = i * kBlock + threadIdx.x;
+      const int x = i * kBlock + tid;
       s_v[b][S::v_at(x / PPR, x % PPR)] = rv[i];
     };
     auto clean_v = [&](int j0) INLINE {
@@ -691,6 +706,33 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     float top[2] = {0.f, 0.f};
     u4 kf[KS];   // K operands of the next step
     auto k_operand = [&](const u4* tk, int x, int ks) INLINE { kf[ks] = tk[S::k_at(32 * x + l32, 2 * ks + half)]; };
+    // a step's scores masked, and its reference: keys from j on
+    auto settle = [&](pf32x16 (&s)[2], int j, bool first = false) INLINE {
+      if (first || j + 32 > min(wave_lo, ke)) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int left = min(lim(c), ke) - j - 4 * half;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[c][i] = 8 * (i / 4) + i % 4 < left ? s[c][i] : -INFINITY;
+          top[c] = s[c][0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top[c] = __builtin_elementwise_maximum(top[c], s[c][i]);
+        }
+      }
+      grown = __ballot(top[0] > m[0] + slack || top[1] > m[1] + slack) != 0;
+      if (grown) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          // a row whose own maximum has not passed stays as it is: no row's result hangs on another's
+          const float both = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
+          const float now = both > m[c] + slack ? both : m[c];
+          alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
+          m[c] = now;
+          mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
+          l[c] *= alpha[c];
+        }
+      }
+    };
     // One step: scores of the next 32 keys (kf) into `next`, the probabilities of the scores in
     // `cur` (pn), the V product of those before (pp), and the K operands of the step after it
     // (rows 32 kx on of tk).  Written out MFMA by MFMA, with what fits beside each: an MFMA takes
@@ -699,7 +741,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     // parts waits for the one before.  Probabilities are rounded to bf16 (to nearest, 2^-8 of each
     // at most); their sum is taken before, in fp32.
     auto step = [&](const u4* tk, int kx, const u4* tv, int vx, pf32x16 (&cur)[2], pf32x16 (&next)[2],
-                    const u4 (&pp)[2][2], u4 (&pn)[2][2], auto beside) INLINE {
+                    const u4 (&pp)[2][2], u4 (&pn)[2][2], int j, auto behind, auto beside) INLINE {
       constexpr int Q = 2 * KS, V = 4 * NB, E = 32;      // MFMAs of each kind, elements of a lane
       constexpr int per = E / (Q + V);                   // elements beside an MFMA
       pbf16x8 vf[2][NB];
@@ -730,17 +772,26 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) next[c][i] = 0.f;
-      each<2 * per>([&](auto e) INLINE { part0(e); });
-      each<per>([&](auto e) INLINE { part1(e); });
       __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the K operands, all in one wait
       __builtin_amdgcn_sched_barrier(0);
       each<Q>([&](auto n) INLINE {
         constexpr int ks = n / 2, c = n % 2, x = n - Q / 2;
+        if constexpr (n == 2) {   // behind the first MFMAs: what would leave the pipe empty before them
+          behind();
+          settle(cur, j);
+          each<2 * per>([&](auto e) INLINE { part0(e); });
+          each<per>([&](auto e) INLINE { part1(e); });
+        }
         next[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pbf16x8, kf[ks]),
                                                           __builtin_bit_cast(pbf16x8, qf[c][ks]), next[c], 0, 0, 0);
         if constexpr (x >= 0 && x < 2 * NB) vf[x / NB][x % NB] = vt(tv, vx, x / NB, x % NB);
-        if constexpr (x < 0) beside(n);
-        elements(n);
+        if constexpr (n == 2 || n == 3) {
+          beside(std::integral_constant<int, n - 2>());
+          elements(std::integral_constant<int, 2 * n - 4>());
+          elements(std::integral_constant<int, 2 * n - 3>());
+        }
+        if constexpr (x < 0 && n >= 2) beside(n);
+        if constexpr (n >= 4) elements(n);
         __builtin_amdgcn_sched_barrier(0);
       });
       each<V>([&](auto n) INLINE {
@@ -764,34 +815,6 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) asm volatile("" : "+v"(pn[kk][c]));
-    };
-    // a step's scores masked, and its reference: keys from j on
-    auto settle = [&](pf32x16 (&s)[2], int j, bool first = false) INLINE {
-      if (first || j + 32 > min(wave_lo, ke)) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int left = min(here(lim[c]), ke) - j - 4 * half;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[c][i] = 8 * (i / 4) + i % 4 < left ? s[c][i] : -INFINITY;
-          top[c] = s[c][0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) top[c] = __builtin_elementwise_maximum(top[c], s[c][i]);
-        }
-      }
-      grown = __ballot(top[0] > pass[0] || top[1] > pass[1]) != 0;
-      if (grown) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          // a row whose own maximum has not passed stays as it is: no row's result hangs on another's
-          const float both = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
-          const float now = both > pass[c] ? both : m[c];
-          alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
-          m[c] = now;
-          mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
-          pass[c] = now + 8.f / a.scale_log2;
-          l[c] *= alpha[c];
-        }
-      }
     };
     auto follow = [&]() INLINE {
       if (grown) {
@@ -866,22 +889,23 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       // tile before, tile b, and the next: three buffers of each, one barrier.
       auto stage = [&](auto buffer, int j0) INLINE {
         constexpr int b = decltype(buffer)::value, b1 = (b + 1) % 3, b2 = (b + 2) % 3;
-        __syncthreads();
-        // a tile's loads right behind the stores of the one before: nearly two steps ahead
-        reach(j0 + 3 * BN);
-        step(s_k[b1], 0, s_v[b2], 1, s0, s1, p1, p0, [&](auto n) INLINE {
-          if constexpr (n < NP) put_k(b2, n);
-          else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
-        });
+        step(s_k[b1], 0, s_v[b2], 1, s0, s1, p1, p0, j0,
+             [&]() INLINE {
+               __syncthreads();
+               reach(j0 + 3 * BN);
+             },
+             // a tile's loads right behind the stores of the one before: nearly two steps ahead
+             [&](auto n) INLINE {
+               if constexpr (n < NP) put_k(b2, n);
+               else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
+             });
         follow();
-        settle(s1, j0 + 32);
-        clean_v(j0 + BN);
-        step(s_k[b1], 1, s_v[b], 0, s1, s0, p0, p1, [&](auto n) INLINE {
-          if constexpr (n < NP) put_v(b1, n);
-          else if constexpr (n < 2 * NP) load_v(n - NP);
-        });
+        step(s_k[b1], 1, s_v[b], 0, s1, s0, p0, p1, j0 + 32, [&]() INLINE { clean_v(j0 + BN); },
+             [&](auto n) INLINE {
+               if constexpr (n < NP) put_v(b1, n);
+               else if constexpr (n < 2 * NP) load_v(n - NP);
+             });
         follow();
-        settle(s0, j0 + 64);
       };
       for (int t = 0; t < steps; t += 6) {
         stage(std::integral_constant<int, 0>(), kb + 32 * t);
@@ -904,18 +928,20 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
 
     __syncthreads();   // s_bad; and K and V are read
     // Out by way of LDS, 32 rows at a time: a lane's 4 outputs of each block make stores of whole
-    // lines there, and straight from registers took 8 us, 4 times as long.
+    // lines there: 4 us, where straight from registers took 8.
     {
       const int lane = lane_here(), l32 = lane % 32, half = lane / 32;
       u4* room = (wave < 2 ? s_k[0] : s_v[0]) + wave % 2 * (32 * D / 4);   // of this wave
       if (__ballot(s_bad[lane % D] < ke || s_bad[D - kWave + lane] < ke)) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int c = 0; c < 2; ++c) {
+          const int sees = lim(c);
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (s_bad[32 * b + 8 * (i / 4) + 4 * half + i % 4] < lim[c]) o[b][c][i] = __builtin_nanf("");
+              if (s_bad[32 * b + 8 * (i / 4) + 4 * half + i % 4] < sees) o[b][c][i] = __builtin_nanf("");
+        }
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
