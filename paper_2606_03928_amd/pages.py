@@ -166,14 +166,26 @@ class PageCache:
         """Bytes that resize and compact take as ws."""
         return max(self._bytes(OP_PAGE_RESIZE), self._bytes(OP_PAGE_COMPACT))
 
+    def _scratch(self, nbytes: int, stream) -> torch.Tensor:
+        """Memory of the stream that will use it: what lay there before was that stream's."""
+        if stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    @staticmethod
+    def _capturing(stream) -> bool:
+        if stream is None:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(stream):
+            return torch.cuda.is_current_stream_capturing()
+
     def _ws(self, ws, nbytes: int, stream):
         """(pointer, bytes, tensor) of the given workspace or a new one."""
         if ws is None:
             if nbytes == 0:
                 return None, 0, None
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            if stream is not None:
-                ws.record_stream(stream)     # allocated on the current stream, used on the given one
+            ws = self._scratch(nbytes, stream)
             return ws.data_ptr(), nbytes, ws
         _require(ws.is_cuda and ws.device == self.device and ws.is_contiguous(),
                  "ws must be a contiguous tensor on the cache's device")
@@ -184,12 +196,11 @@ class PageCache:
     def _state(self, ws, op: int, stream):
         """As _ws, for resize and compact: by default the cache's own, as calls that change one
         cache follow each other in any case.  A captured call takes one of its graph's."""
-        if ws is None and not torch.cuda.is_current_stream_capturing():
+        if ws is None and not self._capturing(stream):
             ws = self._state_ws
             if ws is None:
-                ws = self._state_ws = torch.empty(self.state_workspace_bytes(), dtype=torch.uint8,
-                                                  device=self.device)
-                self._state_home = _stream_ptr(self.device, None)
+                ws = self._state_ws = self._scratch(self.state_workspace_bytes(), stream)
+                self._state_home = _stream_ptr(self.device, stream)
             if _stream_ptr(self.device, stream) != self._state_home:
                 ws.record_stream(stream if stream is not None else torch.cuda.current_stream(self.device))
             return ws.data_ptr(), ws.numel(), ws

@@ -441,6 +441,28 @@ def test_state_workspace_on_other_streams(gpu_lib):
         want = got
 
 
+def test_workspaces_belong_to_the_stream_that_uses_them(gpu_lib, monkeypatch):
+    # memory that another stream's pending work has just given up must not be taken for it
+    c = make([3000, 900], 1, 16, 64, F32, M=200, extra=20, seed=33)
+    q, cu = queries(2, 2, 64, F32, 34), ints([0, 1, 2])
+    assert c.attn_workspace_bytes(2, 2, 1) > 0
+    out, want = torch.empty_like(q).contiguous(), c.attn(q, cu, 1)
+    side, made, empty = torch.cuda.Stream(), [], torch.empty
+
+    def noted(*args, **kw):
+        made.append(torch.cuda.current_stream())
+        return empty(*args, **kw)
+
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", noted)
+    c.attn(q, cu, 1, out=out, stream=side)
+    c.resize(ints([3010, 0]), stream=side)
+    monkeypatch.undo()
+    side.synchronize()
+    assert made == [side, side]
+    assert torch.equal(out, want) and c.length.tolist() == [3010, 0]
+
+
 # --- state --------------------------------------------------------------------------------
 
 
