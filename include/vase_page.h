@@ -86,7 +86,8 @@ size_t vase_page_workspace_bytes(int op, const vase_pages* c, int T, int G, int 
  *   lse[t][a] = ln sum_j exp(q[t][a] . k_j / sqrt(d))
  *
  * over the rows j of head h with j < len[s] and, if causal, j <= len[s] - n_s + i.  A token
- * that sees no row (len[s] < n_s) has out = 0 and lse = -inf.  What rows hold that a token
+ * that sees no row (len[s] < n_s), or only scores of -inf, has out = 0 and lse = -inf; one that
+ * sees a score of +inf or NaN has out = NaN, and lse as the formula gives it.  What rows hold that a token
  * does not see (rows behind len[s], later tokens' rows) does not reach its output, be it
  * infinite or NaN.  Sums and the softmax are in fp32; bf16 caches round the
  * probabilities to bf16 for the product with V.

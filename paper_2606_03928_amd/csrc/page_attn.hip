@@ -179,6 +179,20 @@ __device__ __forceinline__ int lane_here() {
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// exp2((x - top) scale) for x <= top, also where both are infinite: 1
+__device__ __forceinline__ float weight(float x, float top, float scale = 1.f) {
+  return x == top ? 1.f : exp2_((x - top) * scale);
+}
+// what is taken from scores whose maximum is m, in log2 units: finite, so that a score of +inf
+// stays one and the sum with it, and scores of -inf alone count as none
+__device__ __forceinline__ float reference(float m, float scale) {
+  return __builtin_amdgcn_fmed3f(m * scale, -3.4028234663852886e38f, 3.4028234663852886e38f);
+}
+// ln of the sum l of probabilities over 2^m
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;   // NaN stays
+}
+
 // Four outputs of a row from d0 on: the result, or (part: the row's place) a partial.
 template <typename T>
 __device__ __forceinline__ void store4(const AttnArgs& a, float* part, int64_t at, const float (&o)[4]) {
@@ -198,7 +212,7 @@ __device__ __forceinline__ void store4(const AttnArgs& a, float* part, int64_t a
 // its maximum (in scaled log2 units) and sum
 __device__ __forceinline__ void store_ml(const AttnArgs& a, float* part, int64_t row, float m, float l) {
   if (part) *reinterpret_cast<float2*>(part) = make_float2(m, l);
-  else if (a.lse) a.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  else if (a.lse) a.lse[row] = lse_of(m, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -519,7 +533,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
         if (__ballot(top > m)) {
           const float now = fmaxf(m, top);
-          const float alpha = m == -INFINITY ? 0.f : exp2_((m - now) * a.scale_log2);
+          const float alpha = weight(m, now, a.scale_log2);
           m = now;
           l *= alpha;
 #pragma unroll
@@ -527,7 +541,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
         }
-        const float mc = m == -INFINITY ? 0.f : m * a.scale_log2;
+        const float mc = reference(m, a.scale_log2);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[i] = exp2_(__builtin_fmaf(s[i], a.scale_log2, -mc));
@@ -726,9 +740,9 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
           // a row whose own maximum has not passed stays as it is: no row's result hangs on another's
           const float both = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
           const float now = both > m[c] + slack ? both : m[c];
-          alpha[c] = m[c] == -INFINITY ? 0.f : exp2_((m[c] - now) * a.scale_log2);
+          alpha[c] = weight(m[c], now, a.scale_log2);
           m[c] = now;
-          mc[c] = now == -INFINITY ? 0.f : now * a.scale_log2;
+          mc[c] = reference(now, a.scale_log2);
           l[c] *= alpha[c];
         }
       }
@@ -1029,7 +1043,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
     float now = top;
 #pragma unroll
     for (int u = 0; u < U; ++u) now = fmaxf(now, y[u].x);
-    const float old = top == -INFINITY ? 0.f : exp2_(top - now);
+    const float old = weight(top, now);
     top = now;
     l *= old;
 #pragma unroll
@@ -1037,7 +1051,7 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u > last) break;
-      const float f = y[u].x == -INFINITY ? 0.f : exp2_(y[u].x - top);
+      const float f = weight(y[u].x, top);
       l += y[u].y * f;
       x[0] += z[u].x * f;
       x[1] += z[u].y * f;
@@ -1196,7 +1210,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
     if (__ballot(top > m)) {
       const float now = fmaxf(m, top);
-      const float alpha = m == -INFINITY ? 0.f : exp2_((m - now) * a.scale_log2);
+      const float alpha = weight(m, now, a.scale_log2);
       m = now;
       l *= alpha;
 #pragma unroll
@@ -1204,7 +1218,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[b][i] *= alpha;
     }
-    const float mc = m == -INFINITY ? 0.f : m * a.scale_log2;
+    const float mc = reference(m, a.scale_log2);
 #pragma unroll
     for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -1257,7 +1271,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float mw = s_ml[w][r][0];
-      const float f = mw == -INFINITY ? 0.f : exp2_((mw - mm) * a.scale_log2);
+      const float f = weight(mw, mm, a.scale_log2);
       ll += s_ml[w][r][1] * f;
       const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(s_v[w]) + r * D + d0);
       x[0] += y.x * f;
@@ -1303,7 +1317,7 @@ __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
   float top = m;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-  const float f = m == -INFINITY ? 0.f : exp2_(m - top);
+  const float f = weight(m, top);
   float sum = l * f;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
@@ -1317,7 +1331,7 @@ __global__ __launch_bounds__(kBlock) void page_combine_kernel(AttnArgs a) {
   const float mul = sum > 0.f ? 1.f / sum : sum;
 #pragma unroll
   for (int e = 0; e < E; ++e) store_out<T>(static_cast<T*>(a.out) + at * D + E * lane + e, x[e] * mul);
-  if (a.lse && lane == 0) a.lse[at] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
 }
 
 template <typename T, int D>

@@ -1,0 +1,102 @@
+"""Attention over a paged cache whose rows hold infinities and NaN that tokens see: what the
+definition gives, wherever in a tile the row lies and whichever kernel takes the call."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import page_model as pm
+from tests.test_gpu_pages import BF16, DEV, F32, WIDE_TABLE, cumulative, ints, make, queries
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+FORMS = {  # H, G, rows, new tokens, rows of a slot at most
+    "one token": (2, 4, 150, 1, 0),
+    "one token, ranges of keys": (2, 4, 2900, 1, 0),
+    "few tokens": (2, 4, 150, 7, 0),
+    "few tokens, ranges of keys": (2, 4, 2900, 7, 0),
+    "many rows": (40, 4, 330, 130, 0),
+    "many rows, shared out": (2, 3, 2500, 150, WIDE_TABLE),
+}
+
+
+def places(L, n):
+    """Rows whose places in a tile differ: the first, the second half of a tile of 64, one that all
+    tokens see, one that some see, the last."""
+    return [0, 40, 70, L - 1 - n // 2, L - 1]
+
+
+@pytest.fixture(params=[(f, t, d) for f in FORMS for t in (BF16, F32) for d in (64, 128)],
+                ids=lambda p: "%s-%s-d%d" % (p[0], str(p[1])[6:], p[2]))
+def case(request, gpu_lib):
+    form, dtype, d = request.param
+    H, G, L, n, most = FORMS[form]
+    c = make([L], H, 16, d, dtype, M=most // 16 or None, seed=80)
+    q = queries(n, H * G, d, dtype, 81)
+    cu = ints([0, n])
+
+    def attn():
+        lse = torch.empty((n, H * G), device=DEV)
+        return c.attn(q, cu, n, lse=lse), lse
+
+    return c, q, n, L, G, attn
+
+
+def cell(c, row, d0):
+    """The place in a pool of head 1's row and column."""
+    return int(c.table[0, row // 16]), 1, row % 16, d0
+
+
+def head_rows(c, pool, L):
+    """Head 1's rows, in 64 bits on the host."""
+    pages = c.table[0, :pm.pages_for(L, 16)].long()
+    return pool[pages, 1].reshape(-1, c.d)[:L].double().cpu()
+
+
+def scores(c, q, n, L, G):
+    """Head 1's scores [n, G, L] in 64 bits, -inf where unseen."""
+    qs = q[:, G:2 * G].double().cpu()
+    z = torch.einsum("ngd,jd->ngj", qs, head_rows(c, c.k, L)) / math.sqrt(c.d)
+    seen = torch.arange(L) <= (torch.arange(n) + L - n)[:, None]
+    return torch.where(seen[:, None], z, torch.tensor(-INF, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_scores_that_are_not_finite(case, value):
+    """A key with such a value: rows that see it have the log-sum-exp of their scores, NaN and
+    +inf among them, and then an out of NaN; a score of -inf adds nothing."""
+    c, q, n, L, G, attn = case
+    want, want_lse = attn()
+    kk = head_rows(c, c.k, L).numpy()[None]
+    qs = q[:, G:2 * G].double().cpu().numpy()[:, None]
+    _, _, b = pm.attend(qs, kk, kk, L, True)     # of the rows as they were: no key counts less
+    others = [a for a in range(q.shape[1]) if not G <= a < 2 * G]
+    for row in places(L, n):
+        at = cell(c, row, 37)
+        old = c.k[at].clone()
+        c.k[at] = value
+        got, lse = attn()
+        ref = torch.logsumexp(scores(c, q, n, L, G), -1)
+        c.k[at] = old
+        unseen = max(row - (L - n), 0)           # tokens before it
+        assert torch.equal(got[:unseen], want[:unseen]) and torch.equal(lse[:unseen], want_lse[:unseen])
+        assert torch.equal(got[:, others], want[:, others]) and torch.equal(lse[:, others], want_lse[:, others])
+        x, out = lse[:, G:2 * G].double().cpu(), got[:, G:2 * G].cpu()
+        fine = torch.isfinite(ref)
+        assert torch.equal(torch.isnan(x), torch.isnan(ref)) and torch.equal(torch.isposinf(x), torch.isposinf(ref))
+        bound = torch.from_numpy(pm.lse_bound(ref[:, None].numpy(), b, L))[:, 0]
+        assert ((x - ref).abs()[fine] <= bound[fine]).all()
+        assert torch.equal(torch.isfinite(out), fine[..., None].expand_as(out))
+        assert torch.isnan(out[~fine]).all()
+
+
+def test_a_query_that_is_not_finite(case):
+    c, q, n, L, G, attn = case
+    want, want_lse = attn()
+    q[n - 1, 1, 5] = NAN
+    got, lse = attn()
+    assert torch.isnan(got[n - 1, 1]).all() and torch.isnan(lse[n - 1, 1])
+    got[n - 1, 1], lse[n - 1, 1] = want[n - 1, 1], want_lse[n - 1, 1]
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
