@@ -870,7 +870,8 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
       for (int i = 0; i < NP; ++i) {
         put_k(0, i);
         put_v(0, i);
-        put_v(2, i);                // for step 0's product, with probabilities of 0
+        const int x = i * kBlock + tid;   // step 0's product, with probabilities of 0: rows of 0, as
+        s_v[2][S::v_at(x / PPR, x % PPR)] = u4{0, 0, 0, 0};   // an infinity would leave NaN
         rk[i] = rk1[i];
         put_k(1, i);
         at_k[i] = bases.at((kb + BN) / 16 + (i * kBlock + wave * kWave) / (16 * PPR));

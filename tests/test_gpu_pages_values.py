@@ -17,7 +17,7 @@ FORMS = {  # H, G, rows, new tokens, rows of a slot at most
     "one token, ranges of keys": (2, 4, 2900, 1, 0),
     "few tokens": (2, 4, 150, 7, 0),
     "few tokens, ranges of keys": (2, 4, 2900, 7, 0),
-    "many rows": (40, 4, 330, 130, 0),
+    "many rows": (80, 4, 330, 130, 0),
     "many rows, shared out": (2, 3, 2500, 150, WIDE_TABLE),
 }
 
@@ -100,3 +100,33 @@ def test_a_query_that_is_not_finite(case):
     assert torch.isnan(got[n - 1, 1]).all() and torch.isnan(lse[n - 1, 1])
     got[n - 1, 1], lse[n - 1, 1] = want[n - 1, 1], want_lse[n - 1, 1]
     assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+def check_values(case, want, cells):
+    """V's column 37 of head 1 holds `cells` (row -> value): rows have there the sum of those that
+    they see, as every probability is above 0, and all else stands."""
+    c, q, n, L, G, attn = case
+    old = [(cell(c, row, 37), c.v[cell(c, row, 37)].clone()) for row in cells]
+    for row, value in cells.items():
+        c.v[cell(c, row, 37)] = value
+    got, lse = attn()
+    for at, x in old:
+        c.v[at] = x
+    assert torch.equal(lse, want[1])
+    for i in range(n):
+        seen = [x for row, x in cells.items() if row <= i + L - n]
+        if seen:
+            ref = torch.full((G,), sum(seen), dtype=got.dtype, device=DEV)
+            x = got[i, G:2 * G, 37]
+            assert torch.equal(torch.isnan(x), torch.isnan(ref)) and torch.equal(x.nan_to_num(), ref.nan_to_num()), i
+            got[i, G:2 * G, 37] = want[0][i, G:2 * G, 37]
+    assert torch.equal(got, want[0])
+
+
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_values_that_all_tokens_see(case, value):
+    c, q, n, L, G, attn = case
+    want = attn()
+    for row in (0, 40, 70):          # of tiles that every row sees whole
+        check_values(case, want, {row: value})
+    check_values(case, want, {3: INF, 70: value})
