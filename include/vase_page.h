@@ -87,8 +87,10 @@ size_t vase_page_workspace_bytes(int op, const vase_pages* c, int T, int G, int 
  *
  * over the rows j of head h with j < len[s] and, if causal, j <= len[s] - n_s + i.  A token
  * that sees no row (len[s] < n_s), or only scores of -inf, has out = 0 and lse = -inf; one that
- * sees a score of +inf or NaN has out = NaN, and lse as the formula gives it.  What rows hold that a token
- * does not see (rows behind len[s], later tokens' rows) does not reach its output, be it
+ * sees a score of +inf or NaN has out = NaN, and lse as the formula gives it.  Values of V that
+ * are infinite or NaN and seen make an output infinite or NaN as the formula does (where
+ * their probability is 0 in fp32, which of both is unspecified).  What rows hold that a
+ * token does not see (rows behind len[s], later tokens' rows) does not reach its output, be it
  * infinite or NaN.  Sums and the softmax are in fp32; bf16 caches round the
  * probabilities to bf16 for the product with V.
  *

@@ -18,7 +18,8 @@
 // zeroed where they are staged.  A later token's V row may hold an infinity or a NaN, which
 // p = 0 would not keep out of a product: in tiles whose keys not every row sees, V rows are
 // looked through as they are staged, such values go in as 0, and each output column
-// keeps the first key that had one; rows that see that key end with NaN there.
+// keeps the first key that had one of either sign (a NaN counts as both); rows that see that
+// key have the infinity, or of both signs NaN, added at the end.
 #include "page_internal.hpp"
 
 #include <type_traits>
@@ -217,17 +218,41 @@ __device__ __forceinline__ void store_ml(const AttnArgs& a, float* part, int64_t
 
 // ---------------------------------------------------------------------------
 // Values of V that no product with 0 keeps out: taken out of a piece of key `key`'s row
-// (columns col on), the first key of each column noted in first_bad[D].
+// (columns col on), the first key of each column and sign noted in bad.
 // ---------------------------------------------------------------------------
+constexpr int kNoKey = 0x7fffffff;
+template <int D>
+struct BadKeys {
+  int pos[D], neg[D];
+  __device__ __forceinline__ void clear(int tid) {
+    if (tid < D) pos[tid] = neg[tid] = kNoKey;
+  }
+  __device__ __forceinline__ void note(int col, int key, uint32_t fp32) {
+    const bool nan = (fp32 & 0x7fffffffu) > 0x7f800000u;
+    if (nan || !(fp32 >> 31)) atomicMin(&pos[col], key);
+    if (nan || fp32 >> 31) atomicMin(&neg[col], key);
+  }
+  // is there one among the keys below end, in any column; the same in all lanes
+  __device__ __forceinline__ bool any(int end) const {
+    const int lane = threadIdx.x % kWave;
+    int first = min(pos[lane], neg[lane]);
+    if constexpr (D > kWave) first = min(first, min(pos[lane + D - kWave], neg[lane + D - kWave]));
+    return __ballot(first < end) != 0;
+  }
+  // what those below end add to an output: -0, which leaves any output as it is, for none
+  __device__ __forceinline__ float sum(int col, int end) const {
+    return (pos[col] < end ? INFINITY : -0.f) + (neg[col] < end ? -INFINITY : -0.f);
+  }
+};
 __device__ __forceinline__ bool is_bad(uint32_t fp32) { return (fp32 & 0x7fffffffu) >= 0x7f800000u; }
-template <typename T>
-__device__ __forceinline__ void scrub(u4& w, int key, int col, int* first_bad) {
+template <typename T, int D>
+__device__ __forceinline__ void scrub(u4& w, int key, int col, BadKeys<D>& bad) {
   if constexpr (std::is_same<T, float>::value) {
     if (is_bad(w.x) || is_bad(w.y) || is_bad(w.z) || is_bad(w.w)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (is_bad(w[i])) {
-          atomicMin(&first_bad[col + i], key);
+          bad.note(col + i, key, w[i]);
           w[i] = 0;
         }
     }
@@ -241,11 +266,11 @@ __device__ __forceinline__ void scrub(u4& w, int key, int col, int* first_bad) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (is_bad(w[i] << 16)) {
-          atomicMin(&first_bad[col + 2 * i], key);
+          bad.note(col + 2 * i, key, w[i] << 16);
           w[i] &= 0xffff0000u;
         }
         if (is_bad(w[i])) {
-          atomicMin(&first_bad[col + 2 * i + 1], key);
+          bad.note(col + 2 * i + 1, key, w[i] & 0xffff0000u);
           w[i] &= 0xffffu;
         }
       }
@@ -409,7 +434,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
   constexpr int BN = S::BN, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
   static_assert(BN == 32, "one MFMA result of keys");
   __shared__ u4 s_k[2][S::kPieces], s_v[2][S::kPieces];
-  __shared__ int s_bad[D];
+  __shared__ BadKeys<D> s_bad;
   __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int32_t s_cu[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int s_wave[kWaves];
@@ -450,7 +475,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
     const int kb = sg.kt0 * BN;
     const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kTileRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
     const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
-    if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+    s_bad.clear(threadIdx.x);
     __syncthreads();
 
     u4 qf[KS];
@@ -579,7 +604,7 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
           const int d0 = 32 * b + 8 * i + 4 * half;
           float x[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = s_bad[d0 + e] < lim ? __builtin_nanf("") : o[b][4 * i + e] * mul;
+          for (int e = 0; e < 4; ++e) x[e] = o[b][4 * i + e] * mul + s_bad.sum(d0 + e, min(lim, ke));
           store4<float>(a, whole ? nullptr : a.part_o + slot * D + d0, at * D + d0, x);
         }
     }
@@ -606,7 +631,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
   constexpr int BN = S::BN, PPR = S::PPR, NP = S::NP, KS = S::KS, NB = S::NB;
   static_assert(BN == 64, "two steps of 32 keys");
   __shared__ u4 s_k[3][S::kPieces], s_v[3][S::kPieces];
-  __shared__ int s_bad[D];
+  __shared__ BadKeys<D> s_bad;
   __shared__ int s_sum[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int32_t s_cu[SHARES ? kMaxTiles + 1 : 1];
   __shared__ int s_wave[kWaves];
@@ -645,7 +670,7 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     const int ke = (int)min((int64_t)sp.sees(a, (min(r0 + kWideRows, rows) - 1) / a.G), (int64_t)sg.kt1 * BN);
     const int least = sp.sees(a, r0 / a.G);   // keys that all rows see
     const int steps = max((ke - kb + BN - 1) / BN, 0) * 2;   // whole tiles: what lies behind is masked
-    if (tid < D) s_bad[tid] = 0x7fffffff;
+    s_bad.clear(tid);
     __syncthreads();
 
     u4 qf[2][KS];
@@ -947,15 +972,14 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
     {
       const int lane = lane_here(), l32 = lane % 32, half = lane / 32;
       u4* room = (wave < 2 ? s_k[0] : s_v[0]) + wave % 2 * (32 * D / 4);   // of this wave
-      if (__ballot(s_bad[lane % D] < ke || s_bad[D - kWave + lane] < ke)) {
+      if (s_bad.any(ke)) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int sees = lim(c);
+          const int sees = min(lim(c), ke);
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (s_bad[32 * b + 8 * (i / 4) + 4 * half + i % 4] < sees) o[b][c][i] = __builtin_nanf("");
+            for (int i = 0; i < 16; ++i) o[b][c][i] += s_bad.sum(32 * b + 8 * (i / 4) + 4 * half + i % 4, sees);
         }
       }
 #pragma unroll
@@ -1102,7 +1126,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   static_assert(BN * PPR * 16 == kFewRows * D * 4, "a wave's V rows and its O take the same room");
   __shared__ u4 s_v[kWaves][BN * PPR];
   __shared__ float s_ml[kWaves][kFewRows][2];
-  __shared__ int s_bad[D];
+  __shared__ BadKeys<D> s_bad;
 
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -1127,7 +1151,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
   int ke = sp.sees(a, (r0 + rows - 1) / a.G);
   if (split < a.n_split - 1) ke = min(ke, kb + a.keys);
   if (kb >= ke && a.n_split > 1) return;   // combine takes no partial of this range
-  if (threadIdx.x < D) s_bad[threadIdx.x] = 0x7fffffff;
+  s_bad.clear(threadIdx.x);
   __syncthreads();
 
   u4 qf[KS];
@@ -1286,7 +1310,7 @@ __global__ __launch_bounds__(kBlock) void page_few_kernel(AttnArgs a) {
     const bool whole = a.n_split == 1;
     const float mul = !whole ? 1.f : ll > 0.f ? 1.f / ll : ll;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = s_bad[d0 + i] < sp.sees(a, ti) ? __builtin_nanf("") : x[i] * mul;
+    for (int i = 0; i < 4; ++i) x[i] = x[i] * mul + s_bad.sum(d0 + i, min(sp.sees(a, ti), ke));
     store4<T>(a, whole ? nullptr : a.part_o + part * D + d0, at * D + d0, x);
     if (d0 == 0) store_ml(a, whole ? nullptr : a.part_ml + part * 2, at, mm * a.scale_log2, ll);
   }

@@ -130,3 +130,16 @@ def test_values_that_all_tokens_see(case, value):
     for row in (0, 40, 70):          # of tiles that every row sees whole
         check_values(case, want, {row: value})
     check_values(case, want, {3: INF, 70: value})
+
+
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_values_that_some_tokens_see(case, value):
+    c, q, n, L, G, attn = case
+    want = attn()
+    rows = sorted({L - n, L - 1 - n // 2, L - 2, L - 1})
+    for row in rows:
+        check_values(case, want, {row: value})
+    for first in rows[:-1]:          # the tokens between see one of them, those behind both
+        for last in (INF, -INF):
+            check_values(case, want, {first: value, rows[-1]: last})
+    check_values(case, want, {40: INF, rows[0]: value})
