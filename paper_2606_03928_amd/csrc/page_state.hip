@@ -44,7 +44,8 @@ __global__ __launch_bounds__(kBlock) void page_write_kernel(PageView c, const ui
   const int64_t at = (int64_t)c.len[s] - ((int64_t)cu[s + 1] - t);   // of any len: in range or not
   const int row = at < 0 || at >= c.M * c.page ? -1 : (int)at;
   const int q = row < 0 ? 0 : page_of_group(c.div, row / 16);
-  const int p = row < 0 || t < cu[s] ? -1 : c.table[(int64_t)s * c.M + q];
+  // offsets that fall may give a slot that the token is not of
+  const int p = row < 0 || t < cu[s] || t >= cu[s + 1] ? -1 : c.table[(int64_t)s * c.M + q];
   if (!valid_page(c, p)) {
     if (lane == 0) raise(status, VASE_STATUS_PAGE_BAD);
     return;

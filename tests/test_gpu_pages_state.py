@@ -21,3 +21,15 @@ def test_write_of_a_slot_whose_length_is_out_of_range(gpu_lib, length):
     c.write(kn, vn, ints([0, 1, 6, 8]))
     assert model_write(m, kn, vn, [0, 1, 6, 8]) == pm.BAD
     same(c, m, pages.STATUS_PAGE_BAD)
+
+
+def test_write_of_offsets_that_fall_stays_within_the_rows(gpu_lib):
+    # the search for token 5 ends at slot 2, whose tokens the offsets say are 1 .. 2
+    c = make([9, 9, 9, 9], 2, 16, 64, garbage=5.0, seed=92)
+    kn, vn = new_rows(10, 2, 64, BF16, 93)
+    c.write(kn, vn, ints([0, 9, 1, 2, 30]))
+    torch.cuda.synchronize()
+    for s in range(4):
+        for x in (c.k, c.v):
+            assert (x[int(c.table[s, 0]), :, 9:] == 5).all()
+    assert int(c.status) == pages.STATUS_PAGE_BAD
