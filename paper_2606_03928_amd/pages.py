@@ -160,7 +160,9 @@ class PageCache:
 
     def attn_workspace_bytes(self, T: int, G: int, max_new: int, max_len: Optional[int] = None) -> int:
         """Bytes that attn takes as ws for these sizes (0: none)."""
-        return self._bytes(OP_PAGE_ATTN, T, G, max_new, self.M * self.page if max_len is None else max_len)
+        # not by way of _bytes, where a float finds what an equal whole number has left
+        return int(self._lib.vase_page_workspace_bytes(
+            OP_PAGE_ATTN, self._by, T, G, max_new, self.M * self.page if max_len is None else max_len))
 
     def state_workspace_bytes(self) -> int:
         """Bytes that resize and compact take as ws."""

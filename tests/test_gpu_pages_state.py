@@ -1,5 +1,7 @@
 """The paged cache's state on the GPU: bad lengths and offsets, and compactions of many (slot,
 head) pairs, bit for bit against the plain host model."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -33,3 +35,16 @@ def test_write_of_offsets_that_fall_stays_within_the_rows(gpu_lib):
         for x in (c.k, c.v):
             assert (x[int(c.table[s, 0]), :, 9:] == 5).all()
     assert int(c.status) == pages.STATUS_PAGE_BAD
+
+
+def test_workspace_sizes_refuse_floats(gpu_lib):
+    c = make([3000, 900], 1, 16, 64, seed=94)
+    for again in range(2):
+        assert c.attn_workspace_bytes(2, 2, 1) > 0
+        q = new_rows(2, 2, 64, BF16, 95)[0]
+        c.attn(q, ints([0, 1, 2]), 1)
+        for sizes in ((2, 2, 1.0), (2.0, 2, 1), (2, 2.0, 1), (2, 2, 1, 3000.0)):
+            with pytest.raises(ctypes.ArgumentError):
+                c.attn_workspace_bytes(*sizes)
+        with pytest.raises(ctypes.ArgumentError):
+            c.attn(q, ints([0, 1, 2]), 1.0)
