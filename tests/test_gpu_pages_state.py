@@ -48,3 +48,115 @@ def test_workspace_sizes_refuse_floats(gpu_lib):
                 c.attn_workspace_bytes(*sizes)
         with pytest.raises(ctypes.ArgumentError):
             c.attn(q, ints([0, 1, 2]), 1.0)
+
+
+def maps(n_map, H, K, L, seed):
+    """Strictly increasing maps of K rows of L: of every fourth head any rows, the last ones (the
+    farthest way), the first ones (none moves), and one row dropped in the middle."""
+    r = np.random.default_rng(seed).random((n_map, H, L))
+    src = np.sort(np.argsort(r, -1)[..., :K], -1)
+    j = np.arange(K)
+    src[:, 1::4] = j + L - K
+    src[:, 2::4] = j
+    src[:, 3::4] = j + (j >= K // 2) * min(1, L - K)
+    return src.astype(np.int32)
+
+
+MANY = [  # live slots, heads, idle slots, page, K, L
+    (7, 73, 0, 16, 333, 400),        # 511 pairs: chunks by ticket
+    (8, 64, 0, 48, 333, 400),        # 512: whole pairs
+    (9, 57, 1, 64, 320, 321),        # 513; 5 chunks of 64 rows, or 10 of 32
+    (3, 171, 0, 16, 60, 130),        # one chunk, not a whole one
+    (2, 300, 1, 32, 64, 64),         # one, and every row may stay
+    (2, 300, 0, 16, 65, 200),        # two, of one row the last
+    (2, 257, 0, 176, 130, 176),      # three
+    (5, 120, 0, 64, 200, 256),       # four
+    (1, 600, 3, 16, 1, 40),
+    (3, 16, 40, 16, 200, 260),       # a grid for 688 pairs, 48 that live
+    (31, 16, 9, 16, 100, 130),       # and 496
+]
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("live,H,idle,page,K,L", MANY)
+def test_compact_of_many_pairs(gpu_lib, live, H, idle, page, K, L, dtype, d):
+    # lengths that differ, maps of other slots, some slots with the same one
+    lengths = [L + i % 3 for i in range(live)] + [5] * idle
+    c = make(lengths, H, page, d, dtype, seed=100, gap=8)
+    m = model(c)
+    src = maps(max(live - 1, 1), H, K, L, 101)
+    where = [(i * 5 + 1) % len(src) for i in range(live)] + [-1] * idle
+    c.compact(ints(where), ints(src))
+    assert m.compact(where, src) == 0
+    same(c, m)
+
+
+@pytest.mark.parametrize("live,H,K,L", [(3, 2731, 100, 130), (4, 4101, 65, 70), (2, 8192, 33, 40)])
+def test_compact_of_more_pairs_than_workgroups(gpu_lib, live, H, K, L):
+    c = make([L] * live, H, 16, 64, seed=102, extra=1)
+    m = model(c)
+    src = maps(2, H, K, L, 103)
+    where = [i % 2 for i in range(live)]
+    c.compact(ints(where), ints(src))
+    assert m.compact(where, src) == 0
+    same(c, m)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_compact_of_many_pairs_with_shared_pages(gpu_lib, dtype, d):
+    K, L, H = 150, 200, 130
+    c = make([L, 0, 0, L, 0], H, 16, d, dtype, extra=60, seed=104)
+    m = model(c)
+    src = maps(3, H, K, L, 105)
+    for x in (m.fork, lambda p: c.fork(ints(p))):
+        x([-1, 0, 0, -1, 3])
+    for new in ([-1, L + 9, -1, -1, L + 3],):          # two of them grow on pages of their own
+        m.resize(new), c.resize(ints(new))
+    same(c, m)
+    for where in ([-1, 0, 2, 1, 0], [2, -1, -1, -1, -1]):   # 520 pairs, then the one that was left
+        assert m.compact(where, src) == 0
+        c.compact(ints(where), ints(src))
+        same(c, m)
+    src = maps(2, H, 70, K, 106)                       # all of them, on pages that none shares
+    assert m.compact([0, 1, 0, 1, 1], src) == 0
+    c.compact(ints([0, 1, 0, 1, 1]), ints(src))
+    same(c, m)
+
+
+def test_compact_of_many_pairs_captured(gpu_lib):
+    # one graph over a round's state, replayed with other maps and eager rounds between
+    K, B, H, S = 130, 20, 140, 4
+    c = make([K + B] * S, H, 16, 64, seed=107)
+    m = model(c)
+    rng = np.random.default_rng(108)
+    src, where, more = ints(maps(S, H, K, K + B, 109)), ints(range(S)), ints([K + B] * S)
+    ws = torch.empty(c.state_workspace_bytes(), dtype=torch.uint8, device=c.device)
+
+    def step():
+        c.compact(where, src, ws=ws)
+        c.resize(more, ws=ws)
+
+    def model_step():
+        assert m.compact(where.tolist(), src.cpu().numpy()) == 0
+        m.resize([K + B] * S)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    model_step()
+    same(c, m)
+    for i in range(4):
+        src.copy_(ints(maps(S, H, K, K + B, 110 + i)))
+        where.copy_(ints(rng.permutation(S)))
+        g.replay()
+        model_step()
+        same(c, m)
+        if i == 1:
+            step()
+            model_step()
+            same(c, m)
