@@ -143,3 +143,73 @@ def test_values_that_some_tokens_see(case, value):
         for last in (INF, -INF):
             check_values(case, want, {first: value, rows[-1]: last})
     check_values(case, want, {40: INF, rows[0]: value})
+
+
+# --- keys lost or counted twice, in the longest slots ------------------------------------------
+
+LONG = 1_050_037
+DOMINANT = 20.0           # their score; every other key's is 0
+
+
+def long_cache(dtype, d=64, G=4, n=1):
+    """A slot of LONG rows of 0, keys and values, and queries of ones."""
+    pages = LONG // 1024 + 2
+    c = make([1, 0], 1, 1024, d, dtype, M=pages, extra=pages, seed=110, garbage=0.0)
+    c.resize(ints([1, LONG]))
+    q = torch.ones((n + 1, G, d), dtype=dtype, device=DEV)
+    return c, q, ints([0, 1, n + 1])
+
+
+def one_hot_mean(rows, sees, d, left_out=None):
+    """out and lse in 64 bits of a token that sees rows < sees: dominant row i has a one in column
+    i % d.  left_out: dominant rows [a, b) that are not counted."""
+    count = np.zeros(d)
+    for i, row in enumerate(rows):
+        if row < sees and not (left_out and left_out[0] <= i < left_out[1]):
+            count[i % d] += 1
+    # scores of 0 weigh e^-20 beside them
+    total = count.sum() + (sees - count.sum()) * math.exp(-DOMINANT)
+    return count / total, DOMINANT + math.log(total)
+
+
+@pytest.mark.parametrize("n", [1, 17])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_no_key_of_a_million_is_lost(gpu_lib, dtype, n):
+    """Keys at both sides of every multiple of 32 (the borders of tiles, ranges and shares are
+    among them) outweigh the rest, 2051 at a time: losing one or counting it twice shows.
+
+    The bound: a lane sums 8 keys of a tile of 32 (bf16) or 4 of 16 (fp32) of its wave's quarter of
+    a range of ceil(LONG / 64) rows, or half of the keys of the 64 to 65 tiles of 64 (129 of 32) of a share:
+    at most 2112 additions, and 20 more join lanes, waves and ranges: 2132 steps of
+    2^-24, on the sum and on the V product. Scores are exact (d ones of 2.5, over 8); an exponential is
+    off by 2^-22 for the hardware's and 20 x 1.45 x 2^-24 for its argument, probabilities near 1
+    by 2^-8 in bf16 as is the output, once each."""
+    c, q, cu = long_cache(dtype, n=n)
+    d, bf16 = c.d, dtype == BF16
+    pages = c.table[1].long()
+    rel = 2 * 2132 * 2.0 ** -24 + 2 * (2.0 ** -22 + 29 * 2.0 ** -24)
+    rel_out = rel + 2 * 2.0 ** -8 * bf16
+    borders = np.arange(32, LONG, 32)
+    worst = 0.0
+    for part in range(0, 32):
+        rows = np.unique(np.concatenate([borders[part::32] - 1, borders[part::32], [LONG - 1 - n // 2]]))
+        at = torch.from_numpy(rows).to(DEV)
+        place = (pages[at // 1024], 0, at % 1024)
+        c.k[place] = 2.5
+        c.v[place[0], 0, place[2], torch.arange(len(rows), device=DEV) % d] = 1.0
+        lse = torch.empty((n + 1, 4), device=DEV)
+        out = c.attn(q, cu, n, lse=lse)
+        c.k[place], c.v[place] = 0.0, 0.0
+        for i in {0, n // 2, n - 1}:
+            sees = LONG - n + i + 1
+            ref, ref_lse = one_hot_mean(rows, sees, d)
+            got = out[1 + i].double().cpu().numpy()
+            err = np.abs(got - ref) / (rel_out * ref + 1e-9)
+            worst = max(worst, err.max())
+            assert err.max() <= 1, (part, i, err.max(), err.argmax() % d)
+            assert np.abs(lse[1 + i].double().cpu().numpy() - ref_lse).max() <= rel + 20 * 2.0 ** -22
+            # one of them left out is beyond the bound, in its own column
+            lost, _ = one_hot_mean(rows, sees, d, (5, 6))
+            assert (np.abs(lost - ref) / (rel_out * ref + 1e-9)).max() > 1
+    assert int(c.status) == 0
+    print("%.2f of the bound" % worst)
