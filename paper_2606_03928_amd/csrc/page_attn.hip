@@ -290,7 +290,9 @@ __device__ __forceinline__ pbf16x8 read_vt(const u4* base, int byte0, int byte1)
 // The tile kernel (fp32).  A wave keeps 32 query rows (one per lane column) and their O^T in
 // registers; K and V tiles of 32 keys pass through two LDS buffers, the next tile's
 // rows on their way to registers while this one is used.  8 slots of 192 tokens over 2100 rows, 4
-// heads to each of 8 KV heads of 128: 583 us, 86 TFLOP/s of the 153 that a large fp32 product reaches.
+// heads to each of 8 KV heads of 128: 690 us, 73 TFLOP/s of the 153 that a large fp32 product reaches.
+// An operand of K or V is read from LDS, waited for and used by 4 MFMAs, one after the other, and
+// a wave has its SIMD to itself (d 128), so that nothing hides LDS's latency.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct Tile {
@@ -319,8 +321,11 @@ struct Tile {
 // a.shares workgroups and none below kLeastShare triples.  A row tile's beginning and end (Q, the
 // first loads, its output: 11 us, where a key tile takes 1.9) count as kSetup triples before
 // its first: with none a fresh prompt's short tiles made some parts twice as long as others
-// (3200 tokens: 202 us, with 6 under 120).  What a workgroup cannot finish of a row tile (its
-// first and last at most) it leaves as a partial.
+// (3200 tokens: 202 us, with 6 under 120).  The number is bf16's: us with 2, 6 and 12, a mixed
+// step of 16 slots over 600 to 4224 rows 114, 104 and 107 (d 64: 80, 74, 78), two fresh prompts of
+// 1600 tokens 66, 57 and 61 (50, 43, 47).  fp32, whose tiles of 32 keys take longer, would have a
+// smaller one: 432, 452 and 481 (189, 194, 205), two of 1100 tokens 80, 94 and 107 (50, 52, 58).
+// What a workgroup cannot finish of a row tile (its first and last at most) it leaves as a partial.
 constexpr int kMaxTiles = 1023;    // row tiles whose sums a workgroup keeps
 constexpr int kLeastShare = 4;
 constexpr int kSetup = 6;
@@ -619,9 +624,10 @@ __global__ __launch_bounds__(kBlock, tile_waves(D)) void page_tile_kernel(AttnAr
 // step t's exponentials run beside the scores of step t + 1 and the V product of step t - 1.
 // Maxima that grow by less than 2^8 leave the reference alone (a probability is then at most
 // 2^8, its rounding to bf16 relative as before).  4 slots of 2048 tokens over 4096 to 8448 rows, 5
-// heads to each of 8 KV heads of 128: 980 to 1110 us by the card's clock, 1.05 to 0.93
+// heads to each of 8 KV heads of 128: 960 to 1110 us by the card's clock, 1.07 to 0.93
 // PFLOP/s, where a product of 8192^3 reaches 1.15; with 128 rows to a workgroup and two to a
-// CU 1200 to 1390.  What is left is the power limit: the clock falls to 1.9 GHz under it.
+// CU 1200 to 1390; rows of 64 645 us, 0.80 PFLOP/s (half of the MFMAs to an exponential).  The
+// clock falls to 1.9 GHz under the power limit, and pool loads are waited for with LDS's.
 // ---------------------------------------------------------------------------
 constexpr int kWideRows = 64 * kWaves;
 
@@ -934,7 +940,9 @@ __global__ __launch_bounds__(kBlock, 1) void page_wide_kernel(AttnArgs a) {
                __syncthreads();
                reach(j0 + 3 * BN);
              },
-             // a tile's loads right behind the stores of the one before: nearly two steps ahead
+             // a tile's loads right behind the stores of the one before, nearly two steps ahead of
+             // their use. They are flat loads, which the counter of LDS counts too, so that the waits
+             // for LDS in between wait for them as well
              [&](auto n) INLINE {
                if constexpr (n < NP) put_k(b2, n);
                else if constexpr (n < 2 * NP) load_k(j0 + 3 * BN, n - NP);
@@ -1410,7 +1418,10 @@ PageAttnPlan page_attn_plan(const vase_pages& c, int T, int G, int max_new, int 
     p.n_tile = p.by_slot ? c.S : (int)((int64_t)T * G / kFewRows) + slots;
     // V rows past the caches where each is read once, from 2^17 of them on (bf16, d 128: 32 MB): us
     // with plain loads and so, 64 slots of 2000 to 8320 rows 251 and 234, 256 of 500 to 4224 441 and
-    // 419, 8 of 4200 25 and 25; one of 4224, which stays in the caches, 8.3 and 9.3.
+    // 419; one of 4224, which stays in the caches, 8.3 and 9.3.  The other rows, slots of 4000 to 4200
+    // over 8 heads: fp32, d 128, 1 slot 21 and 19, 4 (2^17 rows) 36 and 37, 16 108 and 90, 64 382 and
+    // 346; bf16, d 64, 1 slot 10.5 and 10.9, 4 14.6 and 14.8, 16 30 and 30, 64 110 and 87; fp32, d 64, 1
+    // slot 13 and 14, 4 22 and 21, 16 52 and 52, 64 199 and 181.
     // Not K rows: an operand load takes 64 bytes of each, half of a line (256 slots 492).
     p.once = p.by_slot && (int64_t)slots * c.H * max_len >= 1 << 17;
     // 8 workgroups to a CU, at least 256 keys to a range (512 and 1024 took as long), up to

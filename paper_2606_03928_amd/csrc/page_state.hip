@@ -444,7 +444,7 @@ __device__ __forceinline__ RowMove row_move(const PageView& c, const CompactStat
 // before it whose sources reach into it have said so.  They have lower tickets, so they
 // are with running workgroups, which wait for nothing before they speak: every wait
 // ends.  Bound by HBM: each row is read once and written once.  2304 pairs of 4096 rows of 128
-// (bf16): 1.9 ms, 5.1 TB/s; 40 pairs of 2048 rows: 15 us, 4.5 TB/s.
+// (bf16): 1.9 ms, 5.1 TB/s (a copy kernel reaches 6.2); 32 pairs of 2048 rows: 15 us, 4.4 TB/s.
 template <int PPR>
 __global__ __launch_bounds__(kBlock) void page_compact_kernel(PageView c, const int32_t* __restrict__ map,
                                                               const int32_t* __restrict__ src, int K,

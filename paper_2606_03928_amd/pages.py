@@ -13,10 +13,11 @@ errors are ``ValueError`` (arguments) or :class:`.vase.VaseError` (the library).
   * :meth:`PageCache.compact`  -- the survivors of an eviction round (``vase.select``'s map)
 
 A step of serving: ``resize`` to the new lengths, ``write`` and ``attn`` layer by layer
-(``cache.heads(first, count)`` is one layer's view); every B steps a round: ``score`` and
-``select`` on the rows, then ``compact`` for all heads.  With pages of K + B rows and
-one page to a slot, ``cache.k.view(-1, K + B, d)`` is the static cache that ``vase.score``
-and ``vase.Round`` take.
+(``cache.heads(first, count)`` is one layer's view, made once and kept); every B steps a
+round: a survivor map from ``vase.score`` and ``vase.select``, then ``compact`` for all heads.
+``vase.score`` takes rows that lie together: with pages of K + B rows and one page to a
+slot, ``cache.k.view(-1, K + B, d)`` is the static cache that it and ``vase.Round`` take.  On
+smaller pages the rows are first gathered through the table into such a cache.
 
 Data that only the device knows (lengths, page numbers) is checked there: a call that meets
 a bad value, or too few free pages, ORs a ``STATUS_PAGE_*`` bit into ``status`` (an int32
@@ -142,7 +143,8 @@ class PageCache:
                    status=ints(1) if status else None)
 
     def heads(self, first: int, count: int) -> "PageCache":
-        """The same cache with `count` heads from `first` on (a layer's), for write and attn."""
+        """The same cache with `count` heads from `first` on (a layer's), for write and attn.  To be
+        kept for as long as the cache: making it checks all of the cache's tensors anew."""
         _require(0 <= first and 1 <= count and first + count <= self.H, "heads out of range")
         return _Heads(self, first, count)
 
@@ -233,7 +235,7 @@ class PageCache:
         the split of the work; by default what the table can hold).  q may be a part
         of a wider tensor: any stride from token to token.  lse [T, H * G] float32 takes
         the rows' log-sum-exp.  Returns out [T, H * G, d]; the tokens from cu[S] on, if
-        any, are left as they were (zero in an out made here)."""
+        any, are left as they were (zero in an out made here, by a launch of its own)."""
         stride = _token_rows(q, None, self, "q")
         T, HG, d = q.shape
         G, rest = divmod(HG, self.H)
