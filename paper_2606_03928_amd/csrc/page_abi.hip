@@ -77,8 +77,11 @@ int vase_page_attn(const vase_pages* c, const void* q, int64_t q_stride, const i
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(cu, 4))
     return VASE_ERR_INVALID_ARG;
   const vase::PageAttnPlan plan = vase::page_attn_plan(*c, T, G, max_new, max_len);
-  if ((int64_t)plan.n_tile * c->H > kMaxBlocks / plan.n_split || (int64_t)T * c->H * G > 0x7fffffffLL)
+  const int64_t rows = (int64_t)T * c->H * G;
+  if ((int64_t)plan.n_tile * c->H > kMaxBlocks / plan.n_split || rows > 0x7fffffffLL)
     return VASE_ERR_UNSUPPORTED;
+  // the launch that joins ranges has a wave to each row, padding too
+  if (plan.n_split > 1 && rows > 4 * kMaxBlocks) return VASE_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || ws_bytes < plan.bytes || !aligned(ws, 16))) return VASE_ERR_WORKSPACE;
   return hip_status(vase::launch_page_attn(*c, q, q_stride, cu, T, G, causal, out, lse, ws, plan,
                                            word(dev_status), static_cast<hipStream_t>(stream)));
